@@ -341,7 +341,7 @@ def _held(x):
     """What 4 bits keep of x [..., d] (32 bits in, 32 bits out)."""
     g = x.unflatten(-1, (-1, 64))
     lo, hi = g.amin(-1, keepdim=True), g.amax(-1, keepdim=True)
-    step = ((hi - lo) / 15.0).half().float()
+    step = ((hi - lo) * (1.0 / 15.0)).half().float()
     mid = (lo + 8.0 * step).half().float()
     inv = torch.where(step > 0, 1.0 / step, torch.zeros_like(step))
     code = ((g - mid) * inv).round().clamp(-8, 7)
