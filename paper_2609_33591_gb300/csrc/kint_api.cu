@@ -18,6 +18,7 @@
 #include "../../include/kint_attn.h"
 #include "kint_launch.h"
 #include "kint_params.h"
+#include "serve_params.h"
 
 namespace kint {
 
@@ -483,6 +484,17 @@ cudaError_t traced(const char* name, cudaStream_t s, F&& launch) {
   if (cb) cb(name, 1, s, g_cb_user);
   return e;
 }
+
+}  // namespace
+
+// For the serving entry points (serve_api.cu).
+int serve_device(unsigned** status) { return device_setup(status); }
+int serve_num_sms() { return num_sms(); }
+void serve_hook(const char* kernel, int phase, cudaStream_t s) {
+  if (const kint_launch_cb cb = g_cb) cb(kernel, phase, s, g_cb_user);
+}
+
+namespace {
 
 // The operand copies of one pass, all in one launch.
 struct PrepList {

@@ -1,0 +1,67 @@
+// Number formats of the serving kernels: four consecutive channels of fp32, bfloat16 or
+// fp16 to and from fp32 registers.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cstdint>
+
+namespace kint {
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+template <class E>
+__device__ __forceinline__ E from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+
+// N elements in one (or, past 16 bytes, several) aligned vector accesses.
+template <class E, int N>
+struct alignas((sizeof(E) * N) < 16 ? (sizeof(E) * N) : 16) Vec {
+  E v[N];
+};
+
+// N consecutive channels from x: one vector access when `vec` (the address is a multiple of the vector), else one by one.
+template <class E, int N>
+__device__ __forceinline__ void load_ch(const E* x, bool vec, float (&f)[N]) {
+  if (vec) {
+    const Vec<E, N> a = *reinterpret_cast<const Vec<E, N>*>(x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = to_f32(a.v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = to_f32(x[i]);
+  }
+}
+template <class E, int N>
+__device__ __forceinline__ void store_ch(E* x, bool vec, const float (&f)[N]) {
+  if (vec) {
+    Vec<E, N> a;
+#pragma unroll
+    for (int i = 0; i < N; ++i) a.v[i] = from_f32<E>(f[i]);
+    *reinterpret_cast<Vec<E, N>*>(x) = a;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = from_f32<E>(f[i]);
+  }
+}
+
+// fp16 with saturation instead of an infinity (NaN stays NaN).
+__device__ __forceinline__ __half half_sat(float x) {
+  return __float2half_rn(x > 65504.0f ? 65504.0f : (x < -65504.0f ? -65504.0f : x));
+}
+
+// One rotation, each product and sum rounded by itself (no contraction), so that a value comes out the same bits
+// wherever it is rotated.
+__device__ __forceinline__ void rotate(float& a, float& b, float c, float s) {
+  const float x = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
+  const float y = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
+  a = x;
+  b = y;
+}
+
+}  // namespace kint
