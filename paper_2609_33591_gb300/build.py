@@ -17,7 +17,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libkint.so")
 SOURCES = ["kint_api.cu", "kint_fwd.cu", "kint_bwd.cu", "kint_bwd_dkdv.cu", "kint_bwd_dkdv_rs.cu", "kint_bwd_fused.cu", "kint_probe.cu",
-           "serve_api.cu", "serve_blocks.cu", "serve_rope.cu", "serve_cache.cu", "serve_attn.cu"]
+           "serve_api.cu", "serve_blocks.cu", "serve_rope.cu", "serve_cache.cu", "serve_attn_64.cu",
+           "serve_attn_128.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

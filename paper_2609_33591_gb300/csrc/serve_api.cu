@@ -60,9 +60,11 @@ int check_rotation(const int32_t* pos, const float* table, int max_pos, int rot,
 
 // Launch shape of the attention, from sizes the host knows.
 struct AttnPlan {
-  int G, nt, tiles, max_slabs, per_split, nsplit;
+  int G, nt, tiles, max_slabs, per_split, nsplit, cluster, slab_words, big_words;
   size_t scores, stats, part, count, bytes;  // byte offsets in the workspace, and its size
 };
+constexpr int kScoreWords = 16384;  // 64 KB of scores a block
+constexpr int kBlockSlabs = 32 * kAttnWarps;  // a warp keeps the addresses of 32
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int sinks, int max_new, int max_len) {
@@ -78,19 +80,37 @@ bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int s
   if (window) slabs = std::min(slabs, ((long long)sinks + 15) / 16 + ((long long)window + max_new) / 16 + 2);
   const long long units = (long long)B * kv * tiles;
   if (units > (1 << 30)) return false;
-  // 64 slabs a split, fewer while the grid has less than two CTAs for each of 152 SMs, 8 (one a warp) at least
+  a.tiles = (int)tiles;
+  a.max_slabs = (int)slabs;
+  a.slab_words = rows <= 4 ? 64 : 128 * a.nt;
+  // One launch where a cluster of up to 8 blocks can keep the scores in shared memory, 64 KB a block (two blocks a SM) or,
+  // past what 8 such blocks hold, 128 KB.  More blocks than that takes while the grid is under two for each of 152 SMs
+  // and a block would still have 16 slabs (two a warp).
+  const long long most = std::min(kScoreWords / a.slab_words, kBlockSlabs);
+  int c = 1;
+  while (c < 8 && slabs > c * most) c *= 2;
+  a.cluster = slabs <= c * std::min<long long>(2 * most, kBlockSlabs);
+  if (a.cluster) {
+    while (c < 8 && units * c < 304 && slabs >= 32 * c) c *= 2;
+    a.nsplit = c;
+    a.per_split = (int)((slabs + c - 1) / c);
+    a.big_words = std::max(a.per_split * a.slab_words, kAttnWarps * 8 * a.nt * d);
+    a.scores = a.stats = a.part = a.count = 0;
+    a.bytes = 256;  // (unused)
+    return units * c <= 0x7fffffffll;
+  }
+  // Two launches: 64 slabs a block, fewer while the grid is under two blocks a SM, 8 (one a warp) at least.
   long long per = 64;
   while (per > 8 && units * ((slabs + per - 1) / per) < 304) per >>= 1;
   const long long nsplit = (slabs + per - 1) / per;
   if (units * nsplit > 0x7fffffffll) return false;
-  a.tiles = (int)tiles;
-  a.max_slabs = (int)slabs;
   a.per_split = (int)per;
   a.nsplit = (int)nsplit;
+  a.big_words = 0;
   size_t off = 0;
   auto take = [&](size_t n) { const size_t at = off; off = align256(off + n); return at; };
-  a.scores = take((size_t)units * slabs * a.nt * 128 * 4);
-  a.stats = take((size_t)units * nsplit * a.nt * 8 * 2 * 4);
+  a.scores = take((size_t)units * slabs * a.slab_words * 4);
+  a.stats = take((size_t)units * nsplit * (a.nt * 16 + 2) * 4);
   a.part = take((size_t)units * nsplit * a.nt * 8 * (d + 4) * 4);
   a.count = take((size_t)units * 4);
   a.bytes = off;
@@ -259,14 +279,20 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
     for (int r = 0; r <= Kint; ++r) p.e[r] = (float)std::exp(-(double)tau + r * h);
   }
   p.G = a.G; p.tiles = a.tiles; p.nt = a.nt; p.nsplit = a.nsplit; p.per_split = a.per_split; p.max_slabs = a.max_slabs;
+  p.slab_words = a.slab_words; p.big_words = a.big_words;
+  p.by_tiles = fast_div(a.tiles); p.by_kv = fast_div(cache->kv_heads); p.by_G = fast_div(a.G);
+  const int vec = 4 * elem_size(dtype);
+  p.o_vec = reinterpret_cast<uintptr_t>(out->ptr) % vec == 0 && out->stride_t % 4 == 0 && out->stride_h % 4 == 0;
   char* ws = static_cast<char*>(workspace);
   p.scores = reinterpret_cast<float*>(ws + a.scores);
   p.stats = reinterpret_cast<float*>(ws + a.stats);
   p.part = reinterpret_cast<float*>(ws + a.part);
   p.count = reinterpret_cast<int*>(ws + a.count);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if ((rc = traced("k_attn_scores", s, [&] { return launch_attn_scores(p, s); }))) return rc;
-  return traced("k_attn_values", s, [&] { return launch_attn_values(p, s); });
+  auto launch = [&](int what) { return cache->d == 128 ? launch_attn_128(p, what, s) : launch_attn_64(p, what, s); };
+  if (a.cluster) return traced("k_attn", s, [&] { return launch(ATTN_CLUSTER); });
+  if ((rc = traced("k_attn_scores", s, [&] { return launch(ATTN_SCORES); }))) return rc;
+  return traced("k_attn_values", s, [&] { return launch(ATTN_VALUES); });
 }
 
 }  // extern "C"

@@ -8,6 +8,7 @@
 namespace kint {
 
 constexpr int kMaxRequests = 16384;  // requests of one kint_blocks_extend: two 32-bit prefix sums each in shared memory
+constexpr int kAttnWarps = 8;        // warps of an attention block
 constexpr int kGroup = 64;           // channels that share one (scale, centre) pair of the cache
 
 enum Dtype : int { DT_FP32 = 0, DT_BF16 = 1, DT_FP16 = 2 };
@@ -63,6 +64,17 @@ struct CacheIoP {
   unsigned* status;
 };
 
+// Quotients of 0 <= n < 2^31 by a constant: (umulhi(n, mul) + n) >> shift.
+struct FastDiv {
+  unsigned mul;
+  int shift;
+};
+inline FastDiv fast_div(int d) {
+  int s = 0;
+  while ((1ll << s) < d) ++s;
+  return FastDiv{(unsigned)((((1ll << s) - d) << 32) / d + 1), s};
+}
+
 struct AttnP {
   Heads q, o;
   Cache c;
@@ -74,10 +86,14 @@ struct AttnP {
   float e[KMAX + 2];                 // FWM grid values
   int G, tiles, nt;                  // query heads a kv head; row tiles a (request, kv head); 8-row groups a tile
   int nsplit, per_split, max_slabs;  // splits of the slab list, slabs in each, the longest list
-  float* scores;                     // [unit][max_slabs][nt * 128]
-  float* stats;                      // [unit][nsplit][nt * 8][2]
+  int slab_words;                    // scores kept a slab: 128 nt, or 64 for tiles of at most four rows
+  int big_words;                     // one launch: floats of a block's scores, or of its partial sums where those are more
+  float* scores;                     // [unit][max_slabs][slab_words]
+  float* stats;                      // [unit][nsplit][nt * 16 + 2]: extrema of each row, the largest V scale
   float* part;                       // [unit][nsplit][nt * 8][d + 1]
   int* count;                        // [unit]
+  FastDiv by_tiles, by_kv, by_G;
+  int o_vec;                         // four channels of the output in one access
   unsigned* status;
 };
 
@@ -86,8 +102,28 @@ cudaError_t launch_rope_table(const RopeTableP& p, cudaStream_t s);
 cudaError_t launch_rope(const RopeP& p, int nsm, cudaStream_t s);
 cudaError_t launch_append(const CacheIoP& p, int nsm, cudaStream_t s);
 cudaError_t launch_read(const CacheIoP& p, int nsm, cudaStream_t s);
-cudaError_t launch_attn_scores(const AttnP& p, cudaStream_t s);
-cudaError_t launch_attn_values(const AttnP& p, cudaStream_t s);
+enum AttnKernel : int { ATTN_CLUSTER = 0, ATTN_SCORES = 1, ATTN_VALUES = 2 };
+cudaError_t launch_attn_64(const AttnP& p, int what, cudaStream_t s);
+cudaError_t launch_attn_128(const AttnP& p, int what, cudaStream_t s);
+
+// launch_pdl with thread-block clusters of `cluster` blocks.
+template <class Kern, class... Args>
+cudaError_t launch_pdl_cluster(Kern kern, dim3 grid, dim3 block, int smem, int cluster, cudaStream_t s, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
 
 // From kint_api.cu: the status word of the current device (checks it once), its SM count, and the launch hook.
 int serve_device(unsigned** status);
