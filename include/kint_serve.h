@@ -104,7 +104,7 @@ int kint_rope_table(float* table, int max_pos, int rot, const double* freq, doub
  * with (cos, sin) = table[pos][i]; the rest is copied.  inverse: sin -> -sin, which is the gradient's way back.
  * Outputs may be the inputs themselves (same strides); otherwise they must not overlap.
  *   pos  [B or 1][T] int32 (pos_stride_b elements between batches; 0: one row for all); -1: a padding token, copied.
- * d <= 256, even.
+ * d <= 256, even; at most 2^31 pairs of (token, pair of channels, group of 8 heads).
  */
 int kint_rope(const kint_heads* q, const kint_heads* q_out, const kint_heads* k, const kint_heads* k_out,
               const int32_t* pos, long long pos_stride_b, const float* table, int max_pos, int B, int T, int d, int rot,
@@ -136,7 +136,8 @@ int kint_cache_read(const kint_cache* cache, const int64_t* slots, int tokens, c
  *   anchored at the row's extrema over the keys it sees.
  *   max_new  bound on cu[b + 1] - cu[b]; max_len bound on lens[b] (<= width * block_size): they size the launch and
  *            the workspace; rows or keys past them are left out and flagged.
- *   workspace: kint_cache_attn_workspace_bytes bytes (16-byte aligned)
+ *   workspace: kint_cache_attn_workspace_bytes bytes (16-byte aligned).  256 bytes are asked for, and not touched, where the
+ *            scores fit the shared memory of one launch.
  * Results do not depend on the order in which thread blocks run.
  */
 int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache* cache, const int32_t* table,

@@ -1,8 +1,9 @@
-"""Build libkint.so in-tree with nvcc for sm_103a (no torch extension machinery).
+"""Build libkint.so in-tree with nvcc for sm_103a (no torch extension machinery), and beside it
+the Python module that marshals the serving calls (host code, g++, against torch's headers).
 
-The translation units are compiled in parallel and linked against the
+The translation units are compiled in parallel; the library is linked against the
 shared CUDA runtime (the one PyTorch also loads), with an rpath to the CUDA
-toolkit so the library also loads on its own.
+toolkit so it also loads on its own.
 """
 from __future__ import annotations
 
@@ -10,12 +11,15 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libkint.so")
+EXT = os.path.join(BUILD, "_kint_serve.so")
+EXT_SOURCE = os.path.join(CSRC, "serve_torch.cpp")
 SOURCES = ["kint_api.cu", "kint_fwd.cu", "kint_bwd.cu", "kint_bwd_dkdv.cu", "kint_bwd_dkdv_rs.cu", "kint_bwd_fused.cu", "kint_probe.cu",
            "serve_api.cu", "serve_blocks.cu", "serve_rope.cu", "serve_cache.cu", "serve_attn_64.cu",
            "serve_attn_128.cu"]
@@ -38,9 +42,23 @@ def _inputs():
     return max(os.path.getmtime(p) for p in deps)
 
 
+def _ext_command(out: str) -> list[str]:
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        raise RuntimeError("g++ not found: a C++ compiler is required to build the serving module")
+    libs = os.path.join(home, "lib")
+    return [cxx, "-O2", "-std=c++17", "-shared", "-fPIC", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-I", INCLUDE, "-I", sysconfig.get_paths()["include"], "-I", os.path.join(home, "include"),
+            "-I", os.path.join(home, "include", "torch", "csrc", "api", "include"),
+            "-I", os.path.join(os.path.dirname(_cuda_lib_dir(_nvcc())), "include"), EXT_SOURCE, "-o", out,
+            "-L", libs, f"-Wl,-rpath,{libs}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile (if stale) and return the path of libkint.so."""
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _inputs():
+    if not force and all(os.path.exists(f) and os.path.getmtime(f) >= _inputs() for f in (LIB, EXT)):
         return LIB
     os.makedirs(BUILD, exist_ok=True)
     nvcc = _nvcc()
@@ -52,6 +70,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
         objs.append(obj)
         cmd = [nvcc, *flags, "-c", os.path.join(CSRC, src), "-o", obj]
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    ext_tmp = EXT + f".tmp{os.getpid()}"
+    cmd = _ext_command(ext_tmp)
+    procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     failed = []
     for cmd, pr in procs:
         out, _ = pr.communicate()
@@ -60,7 +81,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         elif verbose and out.strip():
             print(out, file=sys.stderr)
     if failed:
-        for o in objs:
+        for o in (*objs, ext_tmp):
             if os.path.exists(o):
                 os.remove(o)
         raise RuntimeError("libkint build failed:\n" + "\n".join(failed))
@@ -72,8 +93,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if os.path.exists(o):
             os.remove(o)
     if res.returncode != 0:
+        os.remove(ext_tmp)
         raise RuntimeError("libkint link failed:\n" + " ".join(link) + "\n" + res.stdout)
     os.replace(tmp, LIB)
+    os.replace(ext_tmp, EXT)
     return LIB
 
 

@@ -63,7 +63,8 @@ struct AttnPlan {
   int G, nt, tiles, max_slabs, per_split, nsplit, cluster, slab_words, big_words;
   size_t scores, stats, part, count, bytes;  // byte offsets in the workspace, and its size
 };
-constexpr int kScoreWords = 16384;  // 64 KB of scores a block
+constexpr int kBlocksPerSm = 16 / kAttnWarps;          // of at most 128 registers a thread
+constexpr int kScoreWords = 8192;  // 32 KB of scores a block, beside 20 KB of copies in flight
 constexpr int kBlockSlabs = 32 * kAttnWarps;  // a warp keeps the addresses of 32
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -83,15 +84,15 @@ bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int s
   a.tiles = (int)tiles;
   a.max_slabs = (int)slabs;
   a.slab_words = rows <= 4 ? 64 : 128 * a.nt;
-  // One launch where a cluster of up to 8 blocks can keep the scores in shared memory, 64 KB a block (two blocks a SM) or,
-  // past what 8 such blocks hold, 128 KB.  More blocks than that takes while the grid is under two for each of 152 SMs
-  // and a block would still have 16 slabs (two a warp).
+  // One launch where a cluster of up to 8 blocks can keep the scores in shared memory, kScoreWords a block (which leaves
+  // room for kBlocksPerSm blocks) or, past what 8 such blocks hold, twice that.  A block costs about 5 us of latency
+  // whatever it does, so a unit is split further only while all blocks still run at once and each has 16 slabs (two a warp).
   const long long most = std::min(kScoreWords / a.slab_words, kBlockSlabs);
-  int c = 1;
-  while (c < 8 && slabs > c * most) c *= 2;
+  const long long slots = 152ll * (a.nt == 2 && d == 128 ? kBlocksPerSm / 2 : kBlocksPerSm);
+  int c = (int)std::min<long long>((slabs + most - 1) / most, 8);
   a.cluster = slabs <= c * std::min<long long>(2 * most, kBlockSlabs);
   if (a.cluster) {
-    while (c < 8 && units * c < 304 && slabs >= 32 * c) c *= 2;
+    while (2 * c <= 8 && units * c * 2 <= slots && slabs >= 4 * kAttnWarps * c) c *= 2;
     a.nsplit = c;
     a.per_split = (int)((slabs + c - 1) / c);
     a.big_words = std::max(a.per_split * a.slab_words, kAttnWarps * 8 * a.nt * d);
@@ -150,6 +151,7 @@ int kint_blocks_extend(const int32_t* lens, const int32_t* add, int32_t* table, 
   p.slots = slots;
   p.table_stride = table_stride; p.width = width; p.free_len = free_len; p.B = B; p.shift = block_shift(block_size);
   p.tokens = tokens;
+  p.vec = (reinterpret_cast<uintptr_t>(slots) | reinterpret_cast<uintptr_t>(pos) | reinterpret_cast<uintptr_t>(req)) % 16 == 0;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return traced("k_blocks", s, [&] { return launch_blocks(p, serve_num_sms(), s); });
 }
@@ -179,6 +181,8 @@ int kint_rope(const kint_heads* q, const kint_heads* q_out, const kint_heads* k,
     if ((rc = check_heads(h, dtype))) return rc;
   if (q->heads != q_out->heads || k->heads != k_out->heads || q->heads + k->heads < 1) return KINT_ERR_ARG;
   if ((rc = check_rotation(pos, table, max_pos, rot, d))) return rc;
+  // (one work item a chunk of 1 to 16 channels of a token at the least: a 31-bit index)
+  if ((long long)B * T * ((d + 1) / 2 + 1) * ((q->heads + k->heads + 7) / 8) > 0x7fff0000ll) return KINT_ERR_UNSUPPORTED;
   RopeP p;
   if ((rc = serve_device(&p.status))) return rc;
   if (B == 0 || T == 0) return KINT_OK;

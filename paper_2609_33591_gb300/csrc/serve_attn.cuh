@@ -32,6 +32,8 @@
 // mma.sync takes the operands from registers, where the codes are unpacked; tcgen05 would want
 // them in shared memory as 16-bit numbers, four times the bytes that the cache holds.
 #pragma once
+#include <atomic>
+
 #include "kint_dev.cuh"
 #include "serve_num.cuh"
 #include "serve_params.h"
@@ -40,6 +42,7 @@ namespace kint {
 namespace {
 
 constexpr int kWarps = kAttnWarps, kThreads = 32 * kWarps;
+constexpr int kMaxGranted = 64;  // devices whose shared-memory grants are remembered
 constexpr float kMasked = -1.0e38f;   // score of a (row, key) that is not visible; a weight of 0 in every form
 constexpr float kNoRow = -0.9e38f;    // a row maximum below it: the row sees nothing
 
@@ -102,8 +105,6 @@ struct Unit {
   int pmin, pmax, low;     // positions of the tile's first and last row; first key of the first row's window
   int nsink, wslab, n;     // slabs of the first tokens; the window's first slab; slabs in all
 };
-
-__device__ __forceinline__ int quot(int n, FastDiv d) { return (int)((__umulhi((unsigned)n, d.mul) + (unsigned)n) >> d.shift); }
 
 __device__ __forceinline__ Unit unit_of(const AttnP& p, int id, int cap, bool& bad) {
   Unit u;
@@ -332,15 +333,16 @@ __device__ __forceinline__ void store_zeros(const AttnP& p, const Unit& u, int D
 // everything down to 2^-38 of the row's maximum is kept; mul = 2^k / sqrt(d); the sums of q 2^-k over each group.
 // Uncentred codes: channels that a word holds at bits 4 are divided by 16, mul carries the codes' 2^24.
 template <int D, int NT, bool F32>
-struct alignas(16) QTile {
-  __half part[F32 ? 2 : 1][8 * NT][D + 8];
+struct QTile {
+  static constexpr int kParts = F32 ? 2 : 1, kBytes = kParts * 8 * NT * (D + 8) * (int)sizeof(__half);
+  __half (*part)[8 * NT][D + 8];  // [kParts], in memory that the key pass takes over once it holds its operands
   float mul[8 * NT];
   float sum[8 * NT][D / kGroup];
   Row row[8 * NT];
 };
 
 template <int D, int NT, bool F32>
-__device__ __forceinline__ void load_qtile(const AttnP& p, const Unit& u, QTile<D, NT, F32>& t) {
+__device__ __forceinline__ void load_qtile(const AttnP& p, const Unit& u, QTile<D, NT, F32>& t, __half (*part)[8 * NT][D + 8]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int N = D / 32;
   for (int r = warp; r < 8 * NT; r += kWarps) {
@@ -365,8 +367,8 @@ __device__ __forceinline__ void load_qtile(const AttnP& p, const Unit& u, QTile<
       s += y;
       if (!F32 && (ch & 1)) y *= 0.0625f;  // odd nibbles sit at bits 4
       const __half hi = __float2half_rn(y);
-      t.part[0][r][ch] = hi;
-      if constexpr (F32) t.part[1][r][ch] = __float2half_rn(y - __half2float(hi));
+      part[0][r][ch] = hi;
+      if constexpr (F32) part[1][r][ch] = __float2half_rn(y - __half2float(hi));
     }
     // 16 * 4 (d = 128) or 32 * 2 (d = 64) channels a group
 #pragma unroll
@@ -380,14 +382,7 @@ __device__ __forceinline__ void load_qtile(const AttnP& p, const Unit& u, QTile<
   }
 }
 
-// The larger of two, NaN if either is: a NaN score makes its row's maximum, and with it the row, NaN.
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-
-// What the key pass leaves besides the scores: per row the largest and smallest score, and the largest V scale.
+// What the key pass leaves besides the scores: per row the largest (NaN where a score is) and smallest score, and the largest V scale.
 template <int NT>
 struct Extrema {
   float hi[NT][2], lo[NT][2];  // rows 8 n + 2 t + c of this lane
@@ -426,6 +421,7 @@ __device__ __forceinline__ void key_pass(const AttnP& p, const Unit& u, const QT
       e.hi[n][c] = kMasked;
       e.lo[n][c] = INFINITY;
     }
+  __syncthreads();  // the scores may lie over qt.part
   const bool four = NT == 1 && p.slab_words == 64, keep = !four || t < 2;
   const int out0 = score_row(2 * t, four), out1 = score_row(2 * t + 1, four);
   float* out = scores + (size_t)warp_id_uniform() * p.slab_words;
@@ -848,7 +844,7 @@ __device__ __forceinline__ float4 peer_f32x4(uint32_t a) {
 }
 
 template <int D, int NT, bool F32, int MODE>
-__global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 1 : 2) k_attn(const __grid_constant__ AttnP p) {
+__global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8 / kWarps)) k_attn(const __grid_constant__ AttnP p) {
   constexpr int R = 8 * NT, V = D / 4;
   extern __shared__ float4 sm4[];
   float* big = reinterpret_cast<float*>(sm4) + Ring<D>::kBytes / 4;  // scores [chunk][slab_words], then partial sums [kWarps][R][D]
@@ -875,7 +871,8 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 1 : 2) k_att
   const Ring<D> ring(sm4);
   {
     ring.template prime<true>(sh);
-    load_qtile<D, NT, F32>(p, u, qt);
+    if (threadIdx.x == 0) qt.part = reinterpret_cast<__half (*)[R][D + 8]>(big);
+    load_qtile<D, NT, F32>(p, u, qt, reinterpret_cast<__half (*)[R][D + 8]>(big));
     __syncthreads();
     Extrema<NT> e;
     key_pass<D, NT, F32, MODE == M_GRID>(p, u, qt, sh, ring, i0, big, e);
@@ -916,8 +913,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 1 : 2) k_att
   if (threadIdx.x < R) bw[threadIdx.x] = block_weight<D, NT>(sums, threadIdx.x);
   cluster_arrive();
   cluster_wait();
-  for (int x = rank * kThreads / C + threadIdx.x; x < u.rows * V; x += kThreads) {
-    if (threadIdx.x >= kThreads / C) break;
+  for (int x = rank + C * threadIdx.x; x < u.rows * V; x += C * kThreads) {
     const int r = x / V;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     float W = 0.0f;
@@ -935,7 +931,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 1 : 2) k_att
 // ---- two launches: scores in the workspace -------------------------------------------------------------
 
 template <int D, int NT, bool F32, bool LOW>
-__global__ void __launch_bounds__(kThreads, 2) k_attn_scores(const __grid_constant__ AttnP p) {
+__global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attn_scores(const __grid_constant__ AttnP p) {
   constexpr int R = 8 * NT;
   extern __shared__ float4 sm4[];
   __shared__ QTile<D, NT, F32> qt;
@@ -954,7 +950,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_attn_scores(const __grid_consta
     const Share sh = share_of(p, u, i0, i1, addr, bad);
     const Ring<D> ring(sm4);
     ring.template prime<true>(sh);
-    load_qtile<D, NT, F32>(p, u, qt);
+    __half (*part)[R][D + 8] = reinterpret_cast<__half (*)[R][D + 8]>(reinterpret_cast<char*>(sm4) + Ring<D>::kBytes);
+    if (threadIdx.x == 0) qt.part = part;
+    load_qtile<D, NT, F32>(p, u, qt, part);
     __syncthreads();
     Extrema<NT> e;
     key_pass<D, NT, F32, LOW>(p, u, qt, sh, ring, i0, p.scores + ((size_t)id * p.max_slabs + i0) * p.slab_words, e);
@@ -967,7 +965,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attn_scores(const __grid_consta
 }
 
 template <int D, int NT, bool F32, int MODE>
-__global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 1 : 2) k_attn_values(const __grid_constant__ AttnP p) {
+__global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8 / kWarps)) k_attn_values(const __grid_constant__ AttnP p) {
   constexpr int R = 8 * NT, V = D / 4;
   extern __shared__ float4 sm4[];
   float* so = reinterpret_cast<float*>(sm4) + Ring<D>::kBytes / 4;  // [kWarps][R][D]
@@ -1074,9 +1072,16 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 1 : 2) k_att
 
 // ---- launches --------------------------------------------------------------------------------------------
 
+// Lets a kernel use `bytes` of dynamic shared memory on the current device; asked of the runtime once a size.
 template <class Kern>
-cudaError_t want_smem(Kern kern, int bytes) {
-  return bytes > 32 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
+cudaError_t want_smem(Kern kern, int bytes, std::atomic<int> (&granted)[kMaxGranted]) {
+  int dev = 0;
+  if (cudaError_t e = cudaGetDevice(&dev)) return e;
+  const bool known = dev >= 0 && dev < kMaxGranted;
+  if (bytes <= 32 * 1024 || (known && granted[dev].load(std::memory_order_relaxed) >= bytes)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && known) granted[dev].store(bytes, std::memory_order_relaxed);
+  return e;
 }
 
 template <int D, int NT, bool F32, int MODE>
@@ -1084,17 +1089,21 @@ cudaError_t go(const AttnP& p, int what, int grid, cudaStream_t s) {
   const int tab = MODE == M_GRID ? (p.calib == CAL_MINMAX ? 8 * NT : 1) * table_len(p.Kint) * (int)sizeof(float2) : 0;
   if (what == ATTN_CLUSTER) {
     const int smem = Ring<D>::kBytes + p.big_words * 4 + tab;
-    if (cudaError_t e = want_smem(k_attn<D, NT, F32, MODE>, smem)) return e;
+    static std::atomic<int> granted[kMaxGranted];
+    if (cudaError_t e = want_smem(k_attn<D, NT, F32, MODE>, smem, granted)) return e;
     return launch_pdl_cluster(k_attn<D, NT, F32, MODE>, dim3(grid), dim3(kThreads), smem, p.nsplit, s, p);
   }
   const int smem = Ring<D>::kBytes + kWarps * 8 * NT * D * (int)sizeof(float) + tab;
-  if (cudaError_t e = want_smem(k_attn_values<D, NT, F32, MODE>, smem)) return e;
+  static std::atomic<int> granted[kMaxGranted];
+  if (cudaError_t e = want_smem(k_attn_values<D, NT, F32, MODE>, smem, granted)) return e;
   return launch_pdl(k_attn_values<D, NT, F32, MODE>, dim3(grid), dim3(kThreads), smem, s, p);
 }
 template <int D, int NT, bool F32, bool LOW>
 cudaError_t go_scores(const AttnP& p, int grid, cudaStream_t s) {
-  if (cudaError_t e = want_smem(k_attn_scores<D, NT, F32, LOW>, Ring<D>::kBytes)) return e;
-  return launch_pdl(k_attn_scores<D, NT, F32, LOW>, dim3(grid), dim3(kThreads), Ring<D>::kBytes, s, p);
+  static std::atomic<int> granted[kMaxGranted];
+  constexpr int smem = Ring<D>::kBytes + QTile<D, NT, F32>::kBytes;
+  if (cudaError_t e = want_smem(k_attn_scores<D, NT, F32, LOW>, smem, granted)) return e;
+  return launch_pdl(k_attn_scores<D, NT, F32, LOW>, dim3(grid), dim3(kThreads), smem, s, p);
 }
 template <int D, int NT, bool F32>
 cudaError_t pick_mode(const AttnP& p, int what, int grid, cudaStream_t s) {

@@ -16,15 +16,21 @@ namespace {
 
 constexpr int kThreads = 1024;
 
-// Inclusive sums of (a, b) over the CTA's threads, 64 bits each; totals in ta, tb.
-__device__ __forceinline__ void cta_scan(long long& a, long long& b, long long& ta, long long& tb, long long (*sh)[32]) {
+// Sums that stop at 2^32 - 1 (still associative): nonsense lengths cannot wrap around.
+__device__ __forceinline__ unsigned add_sat(unsigned a, unsigned b) {
+  const unsigned s = a + b;
+  return s < a ? ~0u : s;
+}
+
+// Inclusive sums of (a, b) over the CTA's threads; the totals in ta, tb.
+__device__ __forceinline__ void cta_scan(unsigned& a, unsigned& b, unsigned& ta, unsigned& tb, unsigned (*sh)[32]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long x = __shfl_up_sync(0xffffffffu, a, o), y = __shfl_up_sync(0xffffffffu, b, o);
+    const unsigned x = __shfl_up_sync(0xffffffffu, a, o), y = __shfl_up_sync(0xffffffffu, b, o);
     if (lane >= o) {
-      a += x;
-      b += y;
+      a = add_sat(a, x);
+      b = add_sat(b, y);
     }
   }
   if (lane == 31) {
@@ -32,26 +38,23 @@ __device__ __forceinline__ void cta_scan(long long& a, long long& b, long long& 
     sh[1][warp] = b;
   }
   __syncthreads();
-  if (warp == 0) {
-    long long x = sh[0][lane], y = sh[1][lane];
+  // every warp sums the warps' totals for itself
+  unsigned x = sh[0][lane], y = sh[1][lane];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
-      if (lane >= o) {
-        x += u;
-        y += v;
-      }
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
+    if (lane >= o) {
+      x = add_sat(x, u);
+      y = add_sat(y, v);
     }
-    sh[0][lane] = x;
-    sh[1][lane] = y;
   }
-  __syncthreads();
+  const unsigned px = __shfl_sync(0xffffffffu, x, (warp + 31) & 31), py = __shfl_sync(0xffffffffu, y, (warp + 31) & 31);
+  ta = __shfl_sync(0xffffffffu, x, 31);
+  tb = __shfl_sync(0xffffffffu, y, 31);
   if (warp > 0) {
-    a += sh[0][warp - 1];
-    b += sh[1][warp - 1];
+    a = add_sat(a, px);
+    b = add_sat(b, py);
   }
-  ta = sh[0][31];
-  tb = sh[1][31];
   __syncthreads();
 }
 
@@ -70,7 +73,7 @@ __device__ __forceinline__ int first_above(const int* incl, int n, int x) {
   return lo;
 }
 
-__device__ __forceinline__ int clamp_int(long long v) { return v > 0x7fffffffll ? 0x7fffffff : (int)v; }
+__device__ __forceinline__ int clamp_int(unsigned v) { return v > 0x7fffffffu ? 0x7fffffff : (int)v; }
 
 struct Req {
   int len, add, held, want;
@@ -94,7 +97,7 @@ __global__ void __launch_bounds__(kThreads) k_blocks(const BlocksP p) {
   extern __shared__ int sm[];
   int* rows = sm;         // [B] inclusive sums of add
   int* need = sm + p.B;   // [B] inclusive sums of the needed blocks
-  __shared__ long long sh[2][32];
+  __shared__ unsigned sh[2][32];
   __shared__ int refused;
   pdl_trigger();
   pdl_wait();
@@ -103,24 +106,24 @@ __global__ void __launch_bounds__(kThreads) k_blocks(const BlocksP p) {
   const int nfree = min(max(__ldg(p.n_free), 0), p.free_len);
   const bool lead = blockIdx.x == 0;
   bool bad = false;
-  long long base_a = 0, base_n = 0;
+  unsigned base_a = 0, base_n = 0;
   for (int b0 = 0; b0 < p.B; b0 += kThreads) {
     const int b = b0 + threadIdx.x;
     Req r = {0, 0, 0, 0};
     if (b < p.B) r = request(p, b, bad);
     const bool fits = r.want <= p.width;
     const int n = fits ? r.want - r.held : 0;
-    long long a = r.add, c = n, ta, tc;
+    unsigned a = (unsigned)r.add, c = (unsigned)n, ta, tc;
     cta_scan(a, c, ta, tc, sh);
-    a += base_a;
-    c += base_n;
-    base_a += ta;
-    base_n += tc;
+    a = add_sat(a, base_a);
+    c = add_sat(c, base_n);
+    base_a = add_sat(base_a, ta);
+    base_n = add_sat(base_n, tc);
     if (b < p.B) {
       rows[b] = clamp_int(a);
       need[b] = clamp_int(c);
       if (lead) {
-        const bool ok = fits && (n == 0 || c <= nfree);
+        const bool ok = fits && (n == 0 || c <= (unsigned)nfree);
         p.cu[b + 1] = clamp_int(a);
         p.lens_out[b] = ok ? r.len + r.add : r.len;
         if (!ok) atomicAdd(&refused, 1);
@@ -128,9 +131,9 @@ __global__ void __launch_bounds__(kThreads) k_blocks(const BlocksP p) {
     }
   }
   __syncthreads();
-  if (base_a > p.tokens) bad = true;
+  if (base_a > (unsigned)p.tokens) bad = true;
   // blocks taken: the needs that fit, in order; the first request that finds too few ends it
-  const int most = base_n < nfree ? (int)base_n : nfree;
+  const int most = base_n < (unsigned)nfree ? (int)base_n : nfree;
   const int gid = blockIdx.x * kThreads + threadIdx.x, gstep = gridDim.x * kThreads;
   for (int k = gid; k < most; k += gstep) {
     const int b = first_above(need, p.B, k);
@@ -139,30 +142,55 @@ __global__ void __launch_bounds__(kThreads) k_blocks(const BlocksP p) {
     const int first = need[b] - (r.want - r.held);
     p.table[(size_t)b * p.table_stride + r.held + (k - first)] = __ldg(p.free_list + nfree - 1 - k);
   }
-  const int live = base_a < p.tokens ? (int)base_a : p.tokens;
-  for (int i = gid; i < p.tokens; i += gstep) {
-    int64_t slot = -1;
-    int pos = -1, req = -1;
-    if (i < live) {
-      req = first_above(rows, p.B, i);
-      const Req r = request(p, req, bad);
-      const int start = rows[req] - r.add;
-      pos = r.len + i - start;
-      const bool fits = r.want <= p.width;
-      const int n = fits ? r.want - r.held : 0;
-      if (fits && (n == 0 || need[req] <= nfree)) {
-        const int at = pos >> p.shift;
-        const int blk = at < r.held ? __ldg(p.table + (size_t)req * p.table_stride + at)
-                                    : __ldg(p.free_list + nfree - 1 - (need[req] - n + at - r.held));
+  // four consecutive tokens a thread: one bisection, one vector a result
+  const int live = base_a < (unsigned)p.tokens ? (int)base_a : p.tokens;
+  for (int i0 = 4 * gid; i0 < p.tokens; i0 += 4 * gstep) {
+    int64_t slot[4];
+    int pos[4], req[4];
+    int q = i0 < live ? first_above(rows, p.B, i0) : p.B, have = -1, start = 0, n = 0;
+    bool ok = false;
+    Req r = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      slot[j] = -1;
+      pos[j] = req[j] = -1;
+      const int i = i0 + j;
+      if (i >= live) continue;
+      while (i >= rows[q]) ++q;
+      if (q != have) {
+        have = q;
+        r = request(p, q, bad);
+        start = rows[q] - r.add;
+        const bool fits = r.want <= p.width;
+        n = fits ? r.want - r.held : 0;
+        ok = fits && (n == 0 || need[q] <= nfree);
+      }
+      pos[j] = r.len + i - start;
+      req[j] = q;
+      if (ok) {
+        const int at = pos[j] >> p.shift;
+        const int blk = at < r.held ? __ldg(p.table + (size_t)q * p.table_stride + at)
+                                    : __ldg(p.free_list + nfree - 1 - (need[q] - n + at - r.held));
         if (blk >= 0)
-          slot = ((int64_t)blk << p.shift) + (pos & ((1 << p.shift) - 1));
+          slot[j] = ((int64_t)blk << p.shift) + (pos[j] & ((1 << p.shift) - 1));
         else
           bad = true;
       }
     }
-    p.slots[i] = slot;
-    p.pos[i] = pos;
-    p.req[i] = req;
+    if (p.vec && i0 + 4 <= p.tokens) {
+      reinterpret_cast<longlong2*>(p.slots + i0)[0] = make_longlong2(slot[0], slot[1]);
+      reinterpret_cast<longlong2*>(p.slots + i0)[1] = make_longlong2(slot[2], slot[3]);
+      *reinterpret_cast<int4*>(p.pos + i0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      *reinterpret_cast<int4*>(p.req + i0) = make_int4(req[0], req[1], req[2], req[3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i0 + j < p.tokens) {
+          p.slots[i0 + j] = slot[j];
+          p.pos[i0 + j] = pos[j];
+          p.req[i0 + j] = req[j];
+        }
+    }
   }
   if (lead && threadIdx.x == 0) {
     p.cu[0] = 0;
@@ -182,9 +210,10 @@ cudaError_t launch_blocks(const BlocksP& p, int nsm, cudaStream_t s) {
     const cudaError_t e = cudaFuncSetAttribute(k_blocks, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
   }
-  int grid = (p.tokens + 2 * kThreads - 1) / (2 * kThreads);
-  grid = grid < 1 ? 1 : (grid > nsm ? nsm : grid);
-  return launch_pdl(k_blocks, dim3(grid), dim3(kThreads), smem, s, p);
+  // 4 tokens a thread, two CTAs a SM
+  long long grid = ((long long)p.tokens + 4 * kThreads - 1) / (4 * kThreads);
+  grid = grid < 1 ? 1 : (grid > 2 * nsm ? 2 * nsm : grid);
+  return launch_pdl(k_blocks, dim3((unsigned)grid), dim3(kThreads), smem, s, p);
 }
 
 }  // namespace kint

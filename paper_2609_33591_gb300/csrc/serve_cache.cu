@@ -1,13 +1,14 @@
 // Writing tokens into the 4-bit cache and reading them back (format: kint_serve.h).
 //
-// A group of 64 channels keeps lo and hi as s = fp16((hi - lo) * (1 / 15)), c = fp16(lo + 8 s)
+// A group of 64 channels keeps lo and hi as s = fp16((hi - lo) / 15), c = fp16(lo + 8 s)
 // and each channel as clamp(rint((x - c) / s), -8, 7): 0.5625 bytes a channel.  Both
 // kernels move each byte once and are bound by HBM on prompts, by latency on one step's
-// tokens.  16 lanes hold a group, four channels each, so its extrema are a 16-lane
-// butterfly and a lane's four codes are the 16 bits the V layout keeps together; a K
-// word is two lanes' codes.
+// tokens.  A lane holds eight channels (one K word, two halves of V words; 16 bytes of a
+// 16-bit input), so a group is eight lanes and its extrema three butterfly steps, and a
+// warp works on 256 channels: two heads of 128, four of 64.  A warp stays with one token:
+// its slot, position and rotation are loaded once for all the heads it takes.
 #include "serve_num.cuh"
-#include "serve_params.h"
+
 #include "tc.cuh"
 
 namespace kint {
@@ -15,201 +16,310 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Rotated channels [e, e + 4) of a row: the pair partners come with a second load (the row is in L1).
-template <class E>
-__device__ __forceinline__ void rotate4(const CacheIoP& p, const E* row, bool vec, int e, int pos, float (&x)[4]) {
+// Where a channel's partner comes from: nowhere (no rotation), the same eight channels (interleaved), eight channels half the
+// rotation away (one vector), or one by one (half layouts that do not split into eights, and unaligned rows).
+enum Layout : int { L_NONE = 0, L_INTER = 1, L_HALF = 2, L_ANY = 3 };
+
+// The rotation of a lane's eight channels: y = x c + partner s, the products and the sum rounded one by one (rotate()).
+struct Turn {
+  float c[8], s[8];
+  int from;       // first channel of the partners (half layout)
+  unsigned mask;  // bit i: channel i is rotated
+};
+
+__device__ __forceinline__ void load_turn(const CacheIoP& p, int e, int pos, Turn& t) {
   const int half = p.rot >> 1;
-  if (e >= p.rot) return;
   const float2* tab = reinterpret_cast<const float2*>(p.table) + (size_t)pos * half;
-  if (p.interleaved) {
+  t.mask = 0;
+  t.from = e < half ? e + half : e - half;
 #pragma unroll
-    for (int i = 0; i < 4; i += 2)
-      if (e + i < p.rot) {
-        const float2 cs = __ldg(tab + ((e + i) >> 1));
-        rotate(x[i], x[i + 1], cs.x, cs.y);
-      }
-    return;
-  }
-  if (half % 4 == 0) {  // the four channels have their partners together
-    const bool low = e < half;
-    float y[4];
-    load_ch<E, 4>(row + (low ? e + half : e - half), vec, y);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 cs = __ldg(tab + (low ? e + i : e + i - half));
-      float a = low ? x[i] : y[i], b = low ? y[i] : x[i];
-      rotate(a, b, cs.x, cs.y);
-      x[i] = low ? a : b;
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 8; ++i) {
     const int ch = e + i;
-    if (ch >= p.rot) continue;
-    const bool low = ch < half;
-    const float2 cs = __ldg(tab + (low ? ch : ch - half));
-    const float y = to_f32(row[low ? ch + half : ch - half]);
-    float a = low ? x[i] : y, b = low ? y : x[i];
-    rotate(a, b, cs.x, cs.y);
-    x[i] = low ? a : b;
+    float2 cs = make_float2(0.0f, 0.0f);
+    if (ch < p.rot) {
+      const bool low = p.interleaved ? (ch & 1) == 0 : ch < half;
+      cs = __ldg(tab + (p.interleaved ? ch >> 1 : (low ? ch : ch - half)));
+      if (low) cs.y = -cs.y;
+      t.mask |= 1u << i;
+    }
+    t.c[i] = cs.x;
+    t.s[i] = cs.y;
   }
 }
 
-// Where row `slot` of kv head h lives: its slab, and the token's place in it.
-__device__ __forceinline__ uint8_t* slab_of(const Cache& c, long long slot, int h, int& j) {
-  const long long blk = slot >> c.shift;
-  const int off = (int)(slot & ((1ll << c.shift) - 1));
-  j = off & 15;
-  return c.pages + blk * c.stride + ((size_t)h * ((1 << c.shift) >> 4) + (off >> 4)) * slab_bytes(c.d);
+template <class E>
+using Chunk = Vec<E, 8>;
+
+// Eight channels of a row as they are, and (half layout) their partners: whole vectors when `vec`, else one by one.
+template <class E>
+__device__ __forceinline__ Chunk<E> fetch(const E* x, bool vec) {
+  Chunk<E> a;
+  if (vec) {
+    a = *reinterpret_cast<const Chunk<E>*>(x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a.v[i] = x[i];
+  }
+  return a;
+}
+template <class E, int LAYOUT>
+__device__ __forceinline__ Chunk<E> fetch_partners(const CacheIoP& p, const E* row, int e, const Turn& t) {
+  if constexpr (LAYOUT == L_HALF) return fetch(row + t.from, true);
+  const int half = p.rot >> 1;
+  Chunk<E> a;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a.v[i] = (t.mask >> i) & 1u ? row[e + i < half ? e + i + half : e + i - half] : from_f32<E>(0.0f);
+  return a;
+}
+template <class E, int LAYOUT>
+__device__ __forceinline__ void turn(const Turn& t, const Chunk<E>& other, float (&x)[8]) {
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float partner = LAYOUT == L_INTER ? x[i ^ 1] : to_f32(other.v[i]);
+    y[i] = __fadd_rn(__fmul_rn(x[i], t.c[i]), __fmul_rn(partner, t.s[i]));
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (t.mask >> i) & 1u ? y[i] : x[i];
 }
 
-// Rows: for each token kv K rows, kv V rows, and the query heads.  32 * 4 channels a warp: one row at d = 128, two
-// at d = 64.
-template <class E, int D>
-__global__ void __launch_bounds__(kThreads) k_append(const CacheIoP p, bool kvec, bool vvec, bool qvec) {
-  constexpr int kLanes = D / 4, kRows = 32 / kLanes;
+// Where a slot's rows live: its token's place in its slab, the slab of head 0, and the bytes from one head to the next.
+struct Place {
+  uint8_t* slab;
+  int j;
+  long long head;
+};
+__device__ __forceinline__ Place place_of(const Cache& c, long long slot, int d) {
+  const int off = (int)(slot & ((1ll << c.shift) - 1));
+  return Place{c.pages + (slot >> c.shift) * c.stride + (size_t)(off >> 4) * slab_bytes(d), off & 15,
+               (long long)slab_bytes(d) << (c.shift - 4)};
+}
+
+constexpr float kRound = 12582912.0f;  // 1.5 * 2^23: adding it rounds to a whole number (to even), kept in the low bits
+
+// Rows a warp works on at once.
+template <int D>
+struct Tile {
+  static constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+};
+
+// Codes of a group's eight channels x, from its s and c.
+struct Packed {
+  uint32_t codes;
+  __half2 scale;
+};
+__device__ __forceinline__ Packed pack8(const float (&x)[8]) {
+  float lo = x[0], hi = x[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    lo = fminf(lo, x[i]);
+    hi = max_nan(hi, x[i]);
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) {
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+  }
+  const bool finite = hi < INFINITY && lo > -INFINITY;  // (a NaN makes hi NaN)
+  const __half sh = finite ? half_sat(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)) : __ushort_as_half(0);
+  const float s = __half2float(sh);
+  const __half ch = finite ? half_sat(__fadd_rn(lo, __fmul_rn(8.0f, s))) : __ushort_as_half(0x7fff);
+  const float c = __half2float(ch), inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+  // codes in the low bits of the rounded sums: code = bits - bits(kRound), 0 .. 15; added up in base 16 mod 2^32
+  uint32_t codes = 0;
+#pragma unroll
+  for (int i = 7; i >= 0; --i) {
+    const float y = fminf(fmaxf(__fmul_rn(__fsub_rn(x[i], c), inv), -8.0f), 7.0f);  // (NaN: -8)
+    codes = codes * 16u + __float_as_uint(__fadd_rn(y, kRound + 8.0f));
+  }
+  return Packed{finite ? codes - 0x4B400000u * 0x11111111u : 0x88888888u, __halves2half2(sh, ch)};
+}
+
+// The rows of one kind (0 K, 1 V, 2 queries) that this warp takes of its token: row groups first, first + warps, ...
+template <class E, int D, int KIND, int LAYOUT>
+__device__ __forceinline__ void token_rows(const CacheIoP& p, const Heads& in, int tok, int first, const Turn& t, const Place& at, bool vec) {
+  constexpr int kLanes = Tile<D>::kLanes, kRows = Tile<D>::kRows;
+  const int lane = threadIdx.x & 31, e = 8 * (lane % kLanes), step = p.warps * kRows;
+  int h = first * kRows + lane / kLanes;
+  const E* row = reinterpret_cast<const E*>(in.p) + tok * in.st + h * in.sh;
+  const long long row_step = step * in.sh;
+  constexpr bool kTurned = KIND != 1 && LAYOUT != L_NONE, kPartners = kTurned && LAYOUT != L_INTER;
+  const bool partners = kPartners && t.mask;
+  uint8_t* slab = at.slab + h * at.head;
+  const int g = (e >> 3) & 7;
+  uint8_t* code = KIND == 0 ? slab + at.j * (D / 2) + (g & 3) * (D / 8) + 4 * (e >> 5)
+                            : slab + 9 * D + 4 * (((at.j >> 1) * 8 + g) * (D / 32) + 2 * (e >> 6)) + 2 * (at.j & 1);
+  uint8_t* scale = slab + (KIND ? 17 * D : 8 * D) + (at.j * (D / kGroup) + e / kGroup) * 4;
+  E* out = KIND == 2 ? reinterpret_cast<E*>(p.qo.p) + tok * p.qo.st + h * p.qo.sh + e : nullptr;
+  for (int h0 = first * kRows; h0 < in.n; h0 += step, h += step) {
+    Chunk<E> cur, other;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) cur.v[i] = other.v[i] = from_f32<E>(0.0f);
+    if (h < in.n) {
+      cur = fetch(row + e, vec);
+      if (partners) other = fetch_partners<E, LAYOUT>(p, row, e, t);
+    }
+    row += row_step;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = to_f32(cur.v[i]);
+    if (kTurned && t.mask) turn<E, LAYOUT>(t, other, x);
+    if constexpr (KIND == 2) {
+      __syncwarp();  // q_out may be q: every partner has been read
+      if (h < in.n) {
+        if (t.mask == 0) {  // as it is, bit for bit
+          if (vec) {
+            *reinterpret_cast<Chunk<E>*>(out) = cur;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[i] = cur.v[i];
+          }
+        } else {
+          store_ch<E, 8>(out, vec, x);
+        }
+      }
+      out += step * p.qo.sh;
+    } else {
+      const Packed k = pack8(x);
+      if (h < in.n) {
+        if constexpr (KIND == 0) {
+          *reinterpret_cast<uint32_t*>(code) = k.codes;
+        } else {
+          reinterpret_cast<uint16_t*>(code)[0] = (uint16_t)k.codes;
+          reinterpret_cast<uint16_t*>(code)[2] = (uint16_t)(k.codes >> 16);
+        }
+        if ((e & (kGroup - 1)) == 0) *reinterpret_cast<__half2*>(scale) = k.scale;
+      }
+      code += step * at.head;
+      scale += step * at.head;
+    }
+  }
+}
+
+template <class E, int D, int LAYOUT>
+__global__ void __launch_bounds__(kThreads, sizeof(E) == 2 ? 5 : 3) k_append(const CacheIoP p, bool kvec, bool vvec, bool qvec) {
+  constexpr int kRows = Tile<D>::kRows;
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, sub = lane / kLanes, e = (lane % kLanes) * 4;
-  const unsigned mask = kRows == 1 ? 0xffffffffu : 0xffffu << (lane & 16);  // the lanes of this row (they branch together)
-  const int nq = p.q.p ? p.q.n : 0, per = 2 * p.c.kv + nq;
-  const long long rows = (long long)p.tokens * per;
-  const long long limit = (long long)p.c.num_blocks << p.c.shift;
-  bool bad = false;
-  const long long warp0 = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 5, step = (long long)gridDim.x * (kThreads >> 5);
-  for (long long r0 = warp0 * kRows; r0 < rows; r0 += step * kRows) {
-    const long long r = r0 + sub;
-    const bool in = r < rows;
-    const int tok = in ? (int)(r / per) : 0, part = in ? (int)(r % per) : 0;
-    const int pos = p.table ? __ldg(p.pos + tok) : -1;
-    const bool turn = pos >= 0 && pos < p.max_pos;
-    if (p.table && !turn && pos != -1) bad = true;
-    if (part >= 2 * p.c.kv) {  // a query row
-      const int h = part - 2 * p.c.kv;
-      const E* src = reinterpret_cast<const E*>(p.q.p) + tok * p.q.st + h * p.q.sh;
-      E* dst = reinterpret_cast<E*>(p.qo.p) + tok * p.qo.st + h * p.qo.sh;
-      float x[4];
-      load_ch<E, 4>(src + e, qvec, x);
-      if (turn) rotate4(p, src, qvec, e, pos, x);
-      __syncwarp(mask);  // q_out may be q: every partner has been read
-      store_ch<E, 4>(dst + e, qvec, x);
-      continue;
-    }
-    const bool isv = part >= p.c.kv;
-    const int h = isv ? part - p.c.kv : part;
-    const Heads& in_h = isv ? p.v : p.k;
-    const bool vec = isv ? vvec : kvec;
-    const E* src = reinterpret_cast<const E*>(in_h.p) + tok * in_h.st + h * in_h.sh;
-    const long long slot = __ldg(p.slots + tok);
-    if (slot >= limit || slot < -1) bad = true;
-    const bool live = in && slot >= 0 && slot < limit;
-    float x[4];
-    load_ch<E, 4>(src + e, vec, x);
-    if (turn && !isv) rotate4(p, src, vec, e, pos, x);
-    float lo = fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), hi = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-    // NaN where a channel is an infinity or a NaN
-    float odd = __fmul_rn(x[0], 0.0f) + __fmul_rn(x[1], 0.0f) + __fmul_rn(x[2], 0.0f) + __fmul_rn(x[3], 0.0f);
-#pragma unroll
-    for (int o = 8; o; o >>= 1) {
-      lo = fminf(lo, __shfl_xor_sync(mask, lo, o));
-      hi = fmaxf(hi, __shfl_xor_sync(mask, hi, o));
-      odd += __shfl_xor_sync(mask, odd, o);
-    }
-    const bool finite = odd == odd;
-    const __half sh = half_sat(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f));
-    const float s = __half2float(sh);
-    const __half ch = finite ? half_sat(__fadd_rn(lo, __fmul_rn(8.0f, s))) : __ushort_as_half(0x7fff);
-    const float c = __half2float(ch);
-    const float inv = s > 0.0f ? __fdiv_rn(1.0f, s) : 0.0f;
-    uint32_t codes = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float y = finite ? __fmul_rn(__fsub_rn(x[i], c), inv) : 0.0f;
-      codes |= (uint32_t)((int)fminf(fmaxf(rintf(y), -8.0f), 7.0f) + 8) << (4 * i);
-    }
-    const uint32_t up = __shfl_xor_sync(mask, codes, 1);
-    if (!live) continue;
-    int j;
-    uint8_t* slab = slab_of(p.c, slot, h, j);
-    if (!isv) {
-      if ((e & 4) == 0)
-        *reinterpret_cast<uint32_t*>(slab + j * (D / 2) + ((e >> 3) & 3) * (D / 8) + 4 * (e >> 5)) = codes | (up << 16);
-    } else {
-      const int g = (e >> 3) & 7, word = ((j >> 1) * 8 + g) * (D / 32) + 2 * (e >> 6) + ((e >> 2) & 1);
-      *reinterpret_cast<uint16_t*>(slab + 9 * D + 4 * word + 2 * (j & 1)) = (uint16_t)codes;
-    }
-    if ((e & (kGroup - 1)) == 0)
-      *reinterpret_cast<__half2*>(slab + (isv ? 17 * D : 8 * D) + (j * (D / kGroup) + (e / kGroup)) * 4) = __halves2half2(sh, ch);
+  const int lane = threadIdx.x & 31, e = 8 * (lane % Tile<D>::kLanes);
+  const int w = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), tok = quot(w, p.by_warps), first = w - tok * p.warps;
+  if (tok >= p.tokens) return;
+  const int nq = p.q.p ? p.q.n : 0, kv = (p.c.kv + kRows - 1) / kRows, all = 2 * kv + (nq + kRows - 1) / kRows;
+  const long long slot = __ldg(p.slots + tok), limit = (long long)p.c.num_blocks << p.c.shift;
+  const int pos = p.table ? __ldg(p.pos + tok) : -1;
+  const bool live = slot >= 0 && slot < limit, turned = pos >= 0 && pos < p.max_pos;
+  if (lane == 0 && ((slot != -1 && !live) || (p.table && pos != -1 && !turned))) dev_flag(p.status, DEV_ERR_BOUNDS);
+  // this warp's first group of each kind: groups K 0 .. kv - 1, V kv .. 2 kv - 1 and queries are numbered through
+  auto from = [&](int base) { return first >= base ? first - base : (p.warps - (base - first) % p.warps) % p.warps; };
+  const int fv = from(kv), fq = from(2 * kv);
+  Turn t;
+  t.mask = 0;
+  t.from = 0;
+  if (LAYOUT != L_NONE && turned && ((live && first < kv) || 2 * kv + fq < all)) load_turn(p, e, pos, t);
+  if (live) {
+    const Place at = place_of(p.c, slot, D);
+    token_rows<E, D, 0, LAYOUT>(p, p.k, tok, first, t, at, kvec);
+    token_rows<E, D, 1, LAYOUT>(p, p.v, tok, fv, t, at, vvec);
   }
-  if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);
+  if (nq) token_rows<E, D, 2, LAYOUT>(p, p.q, tok, fq, t, Place{nullptr, 0, 0}, qvec);
 }
 
-// Rows: for each token kv K rows (when k is asked for), then kv V rows.
+template <class E, int D, bool ISV>
+__device__ __forceinline__ void read_rows(const CacheIoP& p, const Heads& out, int tok, int first, bool live, const Place& at, bool vec) {
+  constexpr int kLanes = Tile<D>::kLanes, kRows = Tile<D>::kRows;
+  const int lane = threadIdx.x & 31, e = 8 * (lane % kLanes), step = p.warps * kRows, g = (e >> 3) & 7;
+  int h = first * kRows + lane / kLanes;
+  const uint8_t* slab = at.slab + h * at.head;
+  const uint8_t* code = ISV ? slab + 9 * D + 4 * (((at.j >> 1) * 8 + g) * (D / 32) + 2 * (e >> 6)) + 2 * (at.j & 1)
+                            : slab + at.j * (D / 2) + (g & 3) * (D / 8) + 4 * (e >> 5);
+  const uint8_t* scale = slab + (ISV ? 17 * D : 8 * D) + (at.j * (D / kGroup) + e / kGroup) * 4;
+  E* dst = reinterpret_cast<E*>(out.p) + tok * out.st + h * out.sh + e;
+  constexpr int kBatch = 4;  // rows whose loads are under way at once
+  for (; h < p.c.kv; h += kBatch * step) {
+    uint32_t codes[kBatch], sc[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      codes[j] = sc[j] = 0;
+      if (live && h + j * step < p.c.kv) {
+        const uint8_t* at_j = code + j * (step * at.head);
+        if constexpr (ISV) {
+          const uint16_t* c = reinterpret_cast<const uint16_t*>(at_j);
+          codes[j] = (uint32_t)__ldg(c) | ((uint32_t)__ldg(c + 2) << 16);
+        } else {
+          codes[j] = __ldg(reinterpret_cast<const uint32_t*>(at_j));
+        }
+        sc[j] = __ldg(reinterpret_cast<const uint32_t*>(scale + j * (step * at.head)));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+      if (h + j * step < p.c.kv) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&sc[j]));
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = live ? __fmaf_rn(f.x, (float)((int)((codes[j] >> (4 * i)) & 15u) - 8), f.y) : 0.0f;
+        store_ch<E, 8>(dst + j * (step * out.sh), vec, x);
+      }
+    code += kBatch * (step * at.head);
+    scale += kBatch * (step * at.head);
+    dst += kBatch * (step * out.sh);
+  }
+}
+
 template <class E, int D>
 __global__ void __launch_bounds__(kThreads) k_read(const CacheIoP p, bool kvec, bool vvec) {
-  constexpr int kLanes = D / 4, kRows = 32 / kLanes;
+  constexpr int kRows = Tile<D>::kRows;
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, sub = lane / kLanes, e = (lane % kLanes) * 4;
-  const int nk = p.k.p ? p.c.kv : 0, nv = p.v.p ? p.c.kv : 0, per = nk + nv;
-  const long long rows = (long long)p.tokens * per;
-  const long long limit = (long long)p.c.num_blocks << p.c.shift;
-  bool bad = false;
-  const long long warp0 = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 5, step = (long long)gridDim.x * (kThreads >> 5);
-  for (long long r = warp0 * kRows + sub; r < rows; r += step * kRows) {
-    const int tok = (int)(r / per), part = (int)(r % per);
-    const bool isv = part >= nk;
-    const int h = isv ? part - nk : part;
-    const long long slot = __ldg(p.slots + tok);
-    if (slot >= limit || slot < -1) bad = true;
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    if (slot >= 0 && slot < limit) {
-      int j;
-      const uint8_t* slab = slab_of(p.c, slot, h, j);
-      const int g = (e >> 3) & 7, word = ((j >> 1) * 8 + g) * (D / 32) + 2 * (e >> 6) + ((e >> 2) & 1);
-      const uint8_t* at = isv ? slab + 9 * D + 4 * word + 2 * (j & 1)
-                              : slab + j * (D / 2) + ((e >> 3) & 3) * (D / 8) + 4 * (e >> 5) + ((e & 4) >> 1);
-      const uint32_t codes = *reinterpret_cast<const uint16_t*>(at);
-      const __half2 sc = *reinterpret_cast<const __half2*>(slab + (isv ? 17 * D : 8 * D) + (j * (D / kGroup) + (e / kGroup)) * 4);
-      const float s = __low2float(sc), c = __high2float(sc);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __fmaf_rn(s, (float)((int)((codes >> (4 * i)) & 15u) - 8), c);
-    }
-    const Heads& out = isv ? p.v : p.k;
-    store_ch<E, 4>(reinterpret_cast<E*>(out.p) + tok * out.st + h * out.sh + e, isv ? vvec : kvec, x);
-  }
-  if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);
+  const int w = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), tok = quot(w, p.by_warps), first = w - tok * p.warps;
+  if (tok >= p.tokens) return;
+  const int per = (p.c.kv + kRows - 1) / kRows, nk = p.k.p ? per : 0;
+  const long long slot = __ldg(p.slots + tok), limit = (long long)p.c.num_blocks << p.c.shift;
+  const bool live = slot >= 0 && slot < limit;
+  if ((threadIdx.x & 31) == 0 && slot != -1 && !live) dev_flag(p.status, DEV_ERR_BOUNDS);
+  const Place at = place_of(p.c, live ? slot : 0, D);
+  const int fv = first >= nk ? first - nk : (p.warps - (nk - first) % p.warps) % p.warps;
+  if (p.k.p) read_rows<E, D, false>(p, p.k, tok, first, live, at, kvec);
+  if (p.v.p) read_rows<E, D, true>(p, p.v, tok, fv, live, at, vvec);
 }
 
-bool vec4(const Heads& h, int esz) {
-  const int bytes = 4 * esz;
-  return h.p && reinterpret_cast<uintptr_t>(h.p) % bytes == 0 && (h.st * esz) % bytes == 0 && (h.sh * esz) % bytes == 0;
+// Whether eight channels of every row make aligned vectors of 16 bytes.
+bool vec8(const Heads& h, int esz) {
+  return h.p && reinterpret_cast<uintptr_t>(h.p) % 16 == 0 && (h.st * esz) % 16 == 0 && (h.sh * esz) % 16 == 0;
 }
 
-int grid_for(long long rows, int per_warp, int nsm) {
-  const long long want = (rows + per_warp * (kThreads / 32) - 1) / (per_warp * (kThreads / 32));
-  const long long most = (long long)nsm * 32;
-  return (int)(want < 1 ? 1 : (want < most ? want : most));
+// Warps a token: enough for 32 a SM, and no more than it has items.
+int warps_for(CacheIoP& p, int items, int nsm) {
+  long long w = ((long long)nsm * 32 + p.tokens - 1) / p.tokens;
+  w = w < 1 ? 1 : (w > items ? items : w);
+  p.warps = (int)w;
+  p.by_warps = fast_div((int)w);
+  const long long blocks = ((long long)p.tokens * w + kThreads / 32 - 1) / (kThreads / 32);
+  return (int)blocks;
 }
 
 template <class E, int D>
-cudaError_t append(const CacheIoP& p, int nsm, cudaStream_t s) {
-  const int esz = (int)sizeof(E);
-  const long long rows = (long long)p.tokens * (2 * p.c.kv + (p.q.p ? p.q.n : 0));
-  return launch_pdl(k_append<E, D>, dim3(grid_for(rows, 128 / D, nsm)), dim3(kThreads), 0, s, p, vec4(p.k, esz), vec4(p.v, esz),
-                    vec4(p.q, esz) && vec4(p.qo, esz));
+cudaError_t append(CacheIoP& p, int nsm, cudaStream_t s) {
+  constexpr int kRows = Tile<D>::kRows;
+  const int esz = (int)sizeof(E), nq = p.q.p ? p.q.n : 0;
+  const int grid = warps_for(p, 2 * ((p.c.kv + kRows - 1) / kRows) + (nq + kRows - 1) / kRows, nsm);
+  const bool kvec = vec8(p.k, esz), vvec = vec8(p.v, esz), qvec = !p.q.p || (vec8(p.q, esz) && vec8(p.qo, esz));
+  if (!p.table) return launch_pdl(k_append<E, D, L_NONE>, dim3(grid), dim3(kThreads), 0, s, p, kvec, vvec, qvec);
+  if (p.interleaved) return launch_pdl(k_append<E, D, L_INTER>, dim3(grid), dim3(kThreads), 0, s, p, kvec, vvec, qvec);
+  if (kvec && qvec && p.rot % 16 == 0) return launch_pdl(k_append<E, D, L_HALF>, dim3(grid), dim3(kThreads), 0, s, p, kvec, vvec, qvec);
+  return launch_pdl(k_append<E, D, L_ANY>, dim3(grid), dim3(kThreads), 0, s, p, kvec, vvec, qvec);
 }
 template <class E, int D>
-cudaError_t read(const CacheIoP& p, int nsm, cudaStream_t s) {
+cudaError_t read(CacheIoP& p, int nsm, cudaStream_t s) {
+  constexpr int kRows = Tile<D>::kRows;
   const int esz = (int)sizeof(E);
-  const long long rows = (long long)p.tokens * p.c.kv * ((p.k.p ? 1 : 0) + (p.v.p ? 1 : 0));
-  return launch_pdl(k_read<E, D>, dim3(grid_for(rows, 128 / D, nsm)), dim3(kThreads), 0, s, p, vec4(p.k, esz), vec4(p.v, esz));
+  const int grid = warps_for(p, ((p.c.kv + kRows - 1) / kRows) * ((p.k.p ? 1 : 0) + (p.v.p ? 1 : 0)), nsm);
+  return launch_pdl(k_read<E, D>, dim3(grid), dim3(kThreads), 0, s, p, vec8(p.k, esz), vec8(p.v, esz));
 }
 
 }  // namespace
 
-cudaError_t launch_append(const CacheIoP& p, int nsm, cudaStream_t s) {
+cudaError_t launch_append(CacheIoP p, int nsm, cudaStream_t s) {
   const bool wide = p.c.d == 128;
   switch (p.dtype) {
     case DT_FP32: return wide ? append<float, 128>(p, nsm, s) : append<float, 64>(p, nsm, s);
@@ -217,7 +327,7 @@ cudaError_t launch_append(const CacheIoP& p, int nsm, cudaStream_t s) {
     default: return wide ? append<__half, 128>(p, nsm, s) : append<__half, 64>(p, nsm, s);
   }
 }
-cudaError_t launch_read(const CacheIoP& p, int nsm, cudaStream_t s) {
+cudaError_t launch_read(CacheIoP p, int nsm, cudaStream_t s) {
   const bool wide = p.c.d == 128;
   switch (p.dtype) {
     case DT_FP32: return wide ? read<float, 128>(p, nsm, s) : read<float, 64>(p, nsm, s);

@@ -5,6 +5,8 @@
 #include <cuda_fp16.h>
 #include <cstdint>
 
+#include "serve_params.h"
+
 namespace kint {
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
@@ -63,5 +65,14 @@ __device__ __forceinline__ void rotate(float& a, float& b, float c, float s) {
   a = x;
   b = y;
 }
+
+// The larger of two, NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+__device__ __forceinline__ int quot(int n, FastDiv d) { return (int)((__umulhi((unsigned)n, d.mul) + (unsigned)n) >> d.shift); }
 
 }  // namespace kint

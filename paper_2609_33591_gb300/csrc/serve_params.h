@@ -8,13 +8,24 @@
 namespace kint {
 
 constexpr int kMaxRequests = 16384;  // requests of one kint_blocks_extend: two 32-bit prefix sums each in shared memory
-constexpr int kAttnWarps = 8;        // warps of an attention block
+constexpr int kAttnWarps = 4;        // warps of an attention block
 constexpr int kGroup = 64;           // channels that share one (scale, centre) pair of the cache
 
 enum Dtype : int { DT_FP32 = 0, DT_BF16 = 1, DT_FP16 = 2 };
 
 // Bytes of one slab: 16 keys of one kv head (K codes, K scales, V codes, V scales).
 __host__ __device__ constexpr int slab_bytes(int d) { return 18 * d; }
+
+// Quotients of 0 <= n < 2^31 by a constant: (umulhi(n, mul) + n) >> shift.
+struct FastDiv {
+  unsigned mul;
+  int shift;
+};
+inline FastDiv fast_div(int d) {
+  int s = 0;
+  while ((1ll << s) < d) ++s;
+  return FastDiv{(unsigned)((((1ll << s) - d) << 32) / d + 1), s};
+}
 
 // A tensor [batch][time][heads][d] in elements of the call's type.
 struct Heads {
@@ -35,6 +46,7 @@ struct BlocksP {
   int32_t *lens_out, *n_free_out, *cu, *pos, *req, *refused;
   int64_t* slots;
   int table_stride, width, free_len, B, shift, tokens;
+  int vec;  // slots, pos and req on 16-byte boundaries
   unsigned* status;
 };
 
@@ -61,19 +73,10 @@ struct CacheIoP {
   const int32_t* pos;
   const float* table;  // null: no rotation
   int max_pos, tokens, rot, interleaved, dtype;
+  int warps;         // warps a token
+  FastDiv by_warps;
   unsigned* status;
 };
-
-// Quotients of 0 <= n < 2^31 by a constant: (umulhi(n, mul) + n) >> shift.
-struct FastDiv {
-  unsigned mul;
-  int shift;
-};
-inline FastDiv fast_div(int d) {
-  int s = 0;
-  while ((1ll << s) < d) ++s;
-  return FastDiv{(unsigned)((((1ll << s) - d) << 32) / d + 1), s};
-}
 
 struct AttnP {
   Heads q, o;
@@ -100,8 +103,8 @@ struct AttnP {
 cudaError_t launch_blocks(const BlocksP& p, int nsm, cudaStream_t s);
 cudaError_t launch_rope_table(const RopeTableP& p, cudaStream_t s);
 cudaError_t launch_rope(const RopeP& p, int nsm, cudaStream_t s);
-cudaError_t launch_append(const CacheIoP& p, int nsm, cudaStream_t s);
-cudaError_t launch_read(const CacheIoP& p, int nsm, cudaStream_t s);
+cudaError_t launch_append(CacheIoP p, int nsm, cudaStream_t s);
+cudaError_t launch_read(CacheIoP p, int nsm, cudaStream_t s);
 enum AttnKernel : int { ATTN_CLUSTER = 0, ATTN_SCORES = 1, ATTN_VALUES = 2 };
 cudaError_t launch_attn_64(const AttnP& p, int what, cudaStream_t s);
 cudaError_t launch_attn_128(const AttnP& p, int what, cudaStream_t s);

@@ -26,85 +26,81 @@ __global__ void k_rope_table(const RopeTableP p) {
 }
 
 // E: element type; N: channels a vector access (1: any stride and alignment); IL: interleaved pairs.
-// A chunk is N pairs: channels [i, i + N) with [i + rot/2, i + rot/2 + N), or the 2 N channels from 2 i when
-// interleaved; the chunks past rot / 2 pairs are 2 N copied channels each.
+// A chunk is two vectors: channels [i, i + N) and [i + rot/2, i + rot/2 + N) of the rotated ones (N pairs in both layouts;
+// element by element, 2 i and 2 i + 1 when interleaved), or two vectors of the copied ones, half their number apart.  So
+// neighbouring threads read neighbouring vectors.  A thread takes the heads hg, hg + groups, ... one after another.  Loading
+// two or four heads before the first store was measured slower (674 MB of bf16: 109 us one at a time, 139, 172): the
+// requests in flight then lie further apart than the memory's open pages.
 template <class E, int N, bool IL>
-__global__ void __launch_bounds__(kThreads) k_rope(const RopeP p, int chunks, int hpt, int hgroups) {
+__global__ void __launch_bounds__(kThreads) k_rope(const RopeP p, FastDiv by_chunks, int chunks, FastDiv by_groups, int groups, FastDiv by_T,
+                                                   int total) {
   pdl_trigger();
   pdl_wait();
+  const int w = blockIdx.x * kThreads + threadIdx.x;
+  if (w >= total) return;
   const int half = p.rot >> 1, turned = half / N;
-  const long long total = (long long)p.B * p.T * hgroups * chunks;
-  bool bad = false;
-  for (long long w = (long long)blockIdx.x * kThreads + threadIdx.x; w < total; w += (long long)gridDim.x * kThreads) {
-    const int ck = (int)(w % chunks);
-    long long x = w / chunks;
-    const int hg = (int)(x % hgroups);
-    x /= hgroups;
-    const int t = (int)(x % p.T), b = (int)(x / p.T);
-    const int pos = __ldg(p.pos + b * p.pos_sb + t);
-    bool turn = ck < turned;
-    if (pos < 0 || pos >= p.max_pos) {
-      bad |= pos != -1;
-      turn = false;
-    }
-    float c[N], s[N];
-    int ia, ib;  // first channels of the two vectors
-    if (ck < turned) {
-      ia = IL ? 2 * N * ck : N * ck;
-      ib = IL ? ia + N : ia + half;
-    } else {
-      ia = p.rot + 2 * N * (ck - turned);
-      ib = ia + N;
-    }
+  const int x = quot(w, by_chunks), ck = w - x * chunks, tok = quot(x, by_groups), hg = x - tok * groups, b = quot(tok, by_T),
+            t = tok - b * p.T;
+  const int pos = __ldg(p.pos + b * p.pos_sb + t);
+  bool turn = ck < turned;
+  if (pos < 0 || pos >= p.max_pos) {
+    if (pos != -1) dev_flag(p.status, DEV_ERR_BOUNDS);
+    turn = false;
+  }
+  float c[N], s[N];
+  int ia, ib;  // first channels of the two vectors
+  if (ck < turned) {
+    ia = IL && N == 1 ? 2 * ck : N * ck;
+    ib = IL && N == 1 ? ia + 1 : ia + half;
+  } else {
+    ia = p.rot + N * (ck - turned);
+    ib = ia + N * (chunks - turned);
+  }
+  // interleaved vectors: pairs N ck / 2 .. and rot / 4 + N ck / 2 ..
+  const float2* tab = reinterpret_cast<const float2*>(p.table) + (size_t)(turn ? pos : 0) * half;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int pair = IL && N > 1 ? N / 2 * ck + (i < N / 2 ? i : half / 2 + i - N / 2) : N * ck + i;
+    const float2 cs = turn ? __ldg(tab + pair) : make_float2(0.0f, 0.0f);
+    c[i] = cs.x;
+    s[i] = p.inverse ? -cs.y : cs.y;
+  }
+  const bool two = ib + N <= p.d;  // the last copied chunk may be one vector
+  const int heads = p.q.n + p.k.n;
+  for (int h = hg; h < heads; h += groups) {
+    const bool isk = h >= p.q.n;
+    const Heads &in = isk ? p.k : p.q, &out = isk ? p.ko : p.qo;
+    const int hh = isk ? h - p.q.n : h;
+    const E* src = reinterpret_cast<const E*>(in.p) + b * in.sb + t * in.st + hh * in.sh;
+    E* dst = reinterpret_cast<E*>(out.p) + b * out.sb + t * out.st + hh * out.sh;
+    Vec<E, N> va = *reinterpret_cast<const Vec<E, N>*>(src + ia), vb;
+    if (two) vb = *reinterpret_cast<const Vec<E, N>*>(src + ib);
     if (turn) {
-      const float2* tab = reinterpret_cast<const float2*>(p.table) + (size_t)pos * half + N * ck;
+      float f[N], g[N];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float2 cs = __ldg(tab + i);
-        c[i] = cs.x;
-        s[i] = p.inverse ? -cs.y : cs.y;
+        f[i] = to_f32(va.v[i]);
+        g[i] = to_f32(vb.v[i]);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) c[i] = s[i] = 0.0f;
-    }
-    const bool two = ib + N <= p.d;  // the last copied chunk may be one vector
-    const int h1 = min((hg + 1) * hpt, p.q.n + p.k.n);
-#pragma unroll 4
-    for (int h = hg * hpt; h < h1; ++h) {
-      const bool isk = h >= p.q.n;
-      const Heads& in = isk ? p.k : p.q;
-      const Heads& out = isk ? p.ko : p.qo;
-      const int hh = isk ? h - p.q.n : h;
-      const E* src = reinterpret_cast<const E*>(in.p) + b * in.sb + t * in.st + hh * in.sh;
-      E* dst = reinterpret_cast<E*>(out.p) + b * out.sb + t * out.st + hh * out.sh;
-      if (!turn) {  // copied as it is, bit for bit
-        const Vec<E, N> a = *reinterpret_cast<const Vec<E, N>*>(src + ia);
-        if (two) {
-          const Vec<E, N> bb = *reinterpret_cast<const Vec<E, N>*>(src + ib);
-          *reinterpret_cast<Vec<E, N>*>(dst + ib) = bb;
-        }
-        *reinterpret_cast<Vec<E, N>*>(dst + ia) = a;
-        continue;
-      }
-      float a[N], bb[N];
-      load_ch<E, N>(src + ia, true, a);
-      load_ch<E, N>(src + ib, true, bb);
       if constexpr (IL && N > 1) {
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
-          rotate(a[2 * i], a[2 * i + 1], c[i], s[i]);
-          rotate(bb[2 * i], bb[2 * i + 1], c[N / 2 + i], s[N / 2 + i]);
+          rotate(f[2 * i], f[2 * i + 1], c[i], s[i]);
+          rotate(g[2 * i], g[2 * i + 1], c[N / 2 + i], s[N / 2 + i]);
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) rotate(a[i], bb[i], c[i], s[i]);
+        for (int i = 0; i < N; ++i) rotate(f[i], g[i], c[i], s[i]);
       }
-      store_ch<E, N>(dst + ia, true, a);
-      store_ch<E, N>(dst + ib, true, bb);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        va.v[i] = from_f32<E>(f[i]);
+        vb.v[i] = from_f32<E>(g[i]);
+      }
     }
+    *reinterpret_cast<Vec<E, N>*>(dst + ia) = va;  // (not turned: as it is, bit for bit)
+    if (two) *reinterpret_cast<Vec<E, N>*>(dst + ib) = vb;
   }
-  if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);
 }
 
 bool heads_vec(const Heads& h, int esz, int bytes) {
@@ -116,17 +112,19 @@ bool heads_vec(const Heads& h, int esz, int bytes) {
 template <class E, int N>
 cudaError_t go(const RopeP& p, int nsm, cudaStream_t s) {
   const int half = p.rot / 2, heads = p.q.n + p.k.n;
-  const int chunks = half / N + (p.d - p.rot + 2 * N - 1) / (2 * N);
+  const int chunks = half / N + ((p.d - p.rot + N - 1) / N + 1) / 2;
   const long long tokens = (long long)p.B * p.T;
   // heads a thread: up to 8, as few as it takes to give every SM four CTAs
   int hpt = 8;
   while (hpt > 1 && tokens * chunks * ((heads + hpt - 1) / hpt) < (long long)nsm * 4 * kThreads) hpt >>= 1;
-  const int hgroups = (heads + hpt - 1) / hpt;
-  const long long work = tokens * chunks * hgroups;
-  const long long want = (work + kThreads - 1) / kThreads;
-  const int grid = (int)(want < (long long)nsm * 32 ? want : (long long)nsm * 32);
-  if (p.interleaved) return launch_pdl(k_rope<E, N, true>, dim3(grid), dim3(kThreads), 0, s, p, chunks, hpt, hgroups);
-  return launch_pdl(k_rope<E, N, false>, dim3(grid), dim3(kThreads), 0, s, p, chunks, hpt, hgroups);
+  const int groups = (heads + hpt - 1) / hpt;
+  const long long work = tokens * chunks * groups;
+  if (work > 0x7fffffffll - kThreads) return cudaErrorInvalidValue;  // (the entry point refuses such sizes)
+  const int grid = (int)((work + kThreads - 1) / kThreads);
+  const FastDiv dc = fast_div(chunks), dg = fast_div(groups), dt = fast_div(p.T);
+  if (p.interleaved)
+    return launch_pdl(k_rope<E, N, true>, dim3(grid), dim3(kThreads), 0, s, p, dc, chunks, dg, groups, dt, (int)work);
+  return launch_pdl(k_rope<E, N, false>, dim3(grid), dim3(kThreads), 0, s, p, dc, chunks, dg, groups, dt, (int)work);
 }
 
 // 16-byte vectors where every address and the pair count allow them, else element by element.

@@ -15,11 +15,14 @@ rotary positions, a training forward and a serving step.
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import math
-from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
+from . import build as _build
 from . import kint
 from .attention import KIntSelfAttention, kint_attention
 
@@ -66,49 +69,36 @@ def load():
     return _lib
 
 
-# ---- arguments ----------------------------------------------------------------------------------
+_mod = None
+
+
+def _ext():
+    """The marshalling module (csrc/serve_torch.cpp): checks, output allocation and the C call, one Python call deep."""
+    global _mod
+    if _mod is None:
+        lib = load()
+        loader = importlib.machinery.ExtensionFileLoader("_kint_serve", _build.EXT)
+        mod = importlib.util.module_from_spec(importlib.util.spec_from_loader("_kint_serve", loader))
+        loader.exec_module(mod)
+        mod.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+            "kint_blocks_extend", "kint_rope", "kint_cache_append", "kint_cache_read", "kint_cache_attn",
+            "kint_cache_attn_workspace_bytes")), kint.KintError)
+        _mod = mod
+    return _mod
+
+
+def _handle(stream):
+    return None if stream is None else stream.cuda_stream
+
 
 def _need(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
 
 
-def _heads(x, what: str, dims: int) -> kint_heads:
-    """[..., heads, d] with contiguous channels on the GPU: (batch,) time, heads, d."""
-    if not (x.is_cuda and x.dim() == dims and x.dtype in DTYPES and (x.stride(-1) == 1 or x.size(-1) == 1)):
-        raise ValueError(f"{what}: expected a CUDA tensor of fp32, bf16 or fp16 with {dims} dimensions and contiguous channels")
-    st = x.stride()
-    return kint_heads(x.data_ptr(), st[0] if dims == 4 else 0, st[-3], st[-2], x.size(-2))
-
-
-def _ints(x, what: str, dtype=torch.int32):
-    if not (x.is_cuda and x.dtype == dtype and (x.dim() == 0 or x.stride(-1) == 1 or x.size(-1) <= 1)):
-        raise ValueError(f"{what}: expected a contiguous CUDA tensor of {dtype}")
-    return x.data_ptr()
-
-
-def _pool(pages) -> kint_cache:
-    """pages [num_blocks, kv_heads, block_size / 16, 18 d], uint8; blocks may be strided."""
-    _need(pages.is_cuda and pages.dtype == torch.uint8 and pages.dim() == 4, "pages: expected a 4-D uint8 CUDA tensor")
-    n, kv, slabs, size = pages.shape
-    _need(size % 18 == 0 and pages.stride()[1:] == (slabs * size, size, 1),
-          "pages: expected [num_blocks, kv_heads, block_size / 16, 18 d], contiguous within a block")
-    return kint_cache(pages.data_ptr(), pages.stride(0), n, 16 * slabs, kv, size // 18)
-
-
-def _stream(stream) -> int:
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
-
-
-def _run(rc: int, what: str):
-    if rc:
-        raise kint.KintError(rc, what)
-
-
 # ---- block tables and slots -----------------------------------------------------------------------
 
-@dataclass
-class BlockPlan:
+class BlockPlan(NamedTuple):
     """One step's rows: lens [B] after it, cu [B + 1] row offsets, and for each new token its slot, position and request."""
     lens: torch.Tensor
     cu: torch.Tensor
@@ -122,18 +112,7 @@ class BlockPlan:
 def extend_blocks(lens, new, table, free, n_free, block_size: int, tokens: int, *, stream=None) -> BlockPlan:
     """Blocks and slots for new[b] more tokens of each request (int32 [B] both).  ``table`` [B, width] gets the blocks
     taken from the end of free[:n_free]; ``tokens`` is the number of places for new tokens (those left over are -1)."""
-    B = lens.shape[0]
-    _need(new.shape == lens.shape and table.dim() == 2 and table.size(0) == B, "lens, new and table disagree on the requests")
-    args = [_ints(x, n) for x, n in ((lens, "lens"), (new, "new"), (table, "table"), (free, "free"), (n_free, "n_free"))]
-    small = torch.empty(2 * B + 3 + 2 * tokens, dtype=torch.int32, device=lens.device)
-    slots = torch.empty(tokens, dtype=torch.int64, device=lens.device)
-    lens_o, cu, n_free_o, refused, pos, req = small.split((B, B + 1, 1, 1, tokens, tokens))
-    at = small.data_ptr()
-    _run(load().kint_blocks_extend(args[0], args[1], args[2], table.stride(0), table.size(1), args[3], free.numel(), args[4], B,
-                                   block_size, tokens, at, at + 4 * (2 * B + 1), at + 4 * B, slots.data_ptr() or 8,
-                                   at + 4 * (2 * B + 3), at + 4 * (2 * B + 3 + tokens), at + 4 * (2 * B + 2), _stream(stream)),
-         "kint_blocks_extend")
-    return BlockPlan(lens_o, cu, slots, pos, req, n_free_o, refused)
+    return BlockPlan(*(_mod or _ext()).extend_blocks(lens, new, table, free, n_free, block_size, tokens, _handle(stream)))
 
 
 # ---- rotary positions -----------------------------------------------------------------------------
@@ -170,38 +149,18 @@ def rope_table(max_pos: int, rot: int, base: float = 10000.0, *, device="cuda", 
     """(cos, sin) pairs [max_pos, rot / 2, 2], fp32 (angles and functions in fp64); keywords as rope_frequencies."""
     freq, mag = rope_frequencies(rot, base, **scaling)
     table = torch.empty(max_pos, rot // 2, 2, dtype=torch.float32, device=device)
-    _run(load().kint_rope_table(table.data_ptr(), max_pos, rot, (ctypes.c_double * len(freq))(*freq), mag, _stream(stream)),
-         "kint_rope_table")
+    handle = torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
+    rc = load().kint_rope_table(table.data_ptr(), max_pos, rot, (ctypes.c_double * len(freq))(*freq), mag, handle)
+    if rc:
+        raise kint.KintError(rc, "kint_rope_table")
     return table
-
-
-def _table(table):
-    _need(table.is_cuda and table.dtype == torch.float32 and table.dim() == 3 and table.size(2) == 2 and table.is_contiguous(),
-          "table: expected a contiguous fp32 CUDA tensor [max_pos, rot / 2, 2]")
-    return table.data_ptr(), table.size(0), 2 * table.size(1)
-
-
-_NO_HEADS = kint_heads(None, 0, 0, 0, 0)
 
 
 def rope(q, k, pos, table, *, interleaved: bool = False, inverse: bool = False, out=None, stream=None):
     """q [B, T, heads, d] and k (or None) rotated to positions pos [B, T] or [T] (int32; -1: left as it is).
     inverse: the opposite rotation, the gradient's way back.  out: (q', k') to write, which may be q and k."""
-    hq = _heads(q, "q", 4)
-    _need(k is None or (k.dtype == q.dtype and k.shape[:2] == q.shape[:2] and k.size(3) == q.size(3)),
-          "q and k disagree on type, batch, time or channels")
-    _need(pos.shape == q.shape[:2] or pos.shape == q.shape[1:2], "pos: expected [B, T] or [T]")
-    tab, max_pos, rot = _table(table)
-    qo, ko = out if out is not None else (torch.empty_like(q), None if k is None else torch.empty_like(k))
-    _need(qo.shape == q.shape and qo.dtype == q.dtype and (k is None or (ko.shape == k.shape and ko.dtype == k.dtype)),
-          "out disagrees with q and k")
-    B, T = q.shape[:2]
-    if q.numel():
-        _run(load().kint_rope(hq, _heads(qo, "out", 4), _NO_HEADS if k is None else _heads(k, "k", 4),
-                              _NO_HEADS if k is None else _heads(ko, "out", 4), _ints(pos, "pos"),
-                              pos.stride(0) if pos.dim() == 2 else 0, tab, max_pos, B, T, q.size(3), rot, interleaved, inverse,
-                              DTYPES[q.dtype], _stream(stream)), "kint_rope")
-    return qo, ko
+    qo, ko = (None, None) if out is None else out
+    return (_mod or _ext()).rope(q, k, pos, table, interleaved, inverse, qo, ko, _handle(stream))
 
 
 class RotaryFn(torch.autograd.Function):
@@ -238,35 +197,12 @@ def cache_pages(num_blocks: int, block_size: int, kv_heads: int, d: int, *, devi
 def append(k, v, slots, pages, *, q=None, pos=None, table=None, interleaved: bool = False, q_out=None, stream=None):
     """New tokens' k and v [tokens, kv_heads, d] into the cache at slots [tokens] (int64; -1: skipped), the keys rotated
     to pos [tokens] where a table is given.  Returns q [tokens, heads, d] rotated likewise (None without q)."""
-    hk, hv = _heads(k, "k", 3), _heads(v, "v", 3)
-    pool = _pool(pages)
-    n = k.size(0)
-    _need(k.shape == v.shape and k.dtype == v.dtype and k.size(2) == pool.d and slots.shape == (n,),
-          "k, v, slots and the pages disagree")
-    _need(table is None or (pos is not None and pos.shape == (n,)), "a rotation needs pos [tokens]")
-    turn = q is not None and table is not None
-    if q is not None:
-        _need(q.dim() == 3 and q.size(0) == n and q.size(2) == pool.d and q.dtype == k.dtype, "q and k disagree")
-        if turn and q_out is None:
-            q_out = torch.empty_like(q)
-    tab, max_pos, rot = _table(table) if table is not None else (None, 0, 0)
-    if n:
-        _run(load().kint_cache_append(pool, hk, hv, _ints(slots, "slots", torch.int64), n, _heads(q, "q", 3) if turn else None,
-                                      _heads(q_out, "q_out", 3) if turn else None, None if table is None else _ints(pos, "pos"),
-                                      tab, max_pos, rot, interleaved, DTYPES[k.dtype], _stream(stream)), "kint_cache_append")
-    return q_out if turn else q
+    return (_mod or _ext()).append(k, v, slots, pages, q, pos, table, interleaved, q_out, _handle(stream))
 
 
 def read(pages, slots, *, dtype=torch.float32, stream=None):
     """Cached keys and values of slots [tokens] as numbers: k, v [tokens, kv_heads, d]; slot -1 gives zeros."""
-    pool = _pool(pages)
-    n = slots.numel()
-    kv = torch.empty(2, n, pool.kv_heads, pool.d, dtype=dtype, device=pages.device)
-    k, v = kv.unbind(0)
-    if n:
-        _run(load().kint_cache_read(pool, _ints(slots, "slots", torch.int64), n, _heads(k, "k", 3), _heads(v, "v", 3),
-                                    DTYPES[dtype], _stream(stream)), "kint_cache_read")
-    return k, v
+    return (_mod or _ext()).read(pages, slots, DTYPES[dtype], _handle(stream))
 
 
 def attention(q, pages, table, lens, cu, cfg: kint.Config, *, window: int = 0, sinks: int = 0, max_new: int | None = None,
@@ -275,26 +211,8 @@ def attention(q, pages, table, lens, cu, cfg: kint.Config, *, window: int = 0, s
     the last positions of its lens[b] cached tokens, whose blocks are table[b].  window > 0: a row sees its last
     ``window`` keys and the first ``sinks``.  max_new and max_len bound the rows a request has and lens (host numbers
     that size the launch; by default rows and what the table can hold)."""
-    hq = _heads(q, "q", 3)
-    pool = _pool(pages)
-    B = lens.size(0)
-    _need(q.size(2) == pool.d and table.dim() == 2 and table.size(0) == B and cu.shape == (B + 1,),
-          "q, pages, table, lens and cu disagree")
-    out = torch.empty_like(q) if out is None else out
-    _need(out.shape == q.shape and out.dtype == q.dtype, "out disagrees with q")
-    if q.numel() == 0:
-        return out
-    width = table.size(1)
-    max_new = q.size(0) if max_new is None else max_new
-    max_len = width * pool.block_size if max_len is None else max_len
-    lib = load()
-    if ws is None:
-        ws = attention_workspace(B, q.size(1), pool.kv_heads, pool.d, window=window, sinks=sinks, max_new=max_new,
-                                 max_len=max_len, device=q.device)
-    _run(lib.kint_cache_attn(hq, _heads(out, "out", 3), pool, _ints(table, "table"), table.stride(0), width, _ints(lens, "lens"),
-                             _ints(cu, "cu"), B, window, sinks, cfg.Kint, cfg.calib, cfg.tau, cfg.recon, max_new, max_len,
-                             DTYPES[q.dtype], ws.data_ptr(), ws.numel(), _stream(stream)), "kint_cache_attn")
-    return out
+    return (_mod or _ext()).attention(q, pages, table, lens, cu, cfg.Kint, cfg.calib, cfg.tau, cfg.recon, window, sinks, max_new,
+                                      max_len, out, ws, _handle(stream))
 
 
 def attention_workspace(B: int, heads: int, kv_heads: int, d: int, *, window: int = 0, sinks: int = 0, max_new: int = 1,
