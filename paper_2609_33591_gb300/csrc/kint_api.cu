@@ -490,6 +490,7 @@ cudaError_t traced(const char* name, cudaStream_t s, F&& launch) {
 // For the serving entry points (serve_api.cu).
 int serve_device(unsigned** status) { return device_setup(status); }
 int serve_num_sms() { return num_sms(); }
+unsigned long long serve_wait_ns() { return g_wait_ns; }
 void serve_hook(const char* kernel, int phase, cudaStream_t s) {
   if (const kint_launch_cb cb = g_cb) cb(kernel, phase, s, g_cb_user);
 }

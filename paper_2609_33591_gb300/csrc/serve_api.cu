@@ -58,15 +58,22 @@ int check_rotation(const int32_t* pos, const float* table, int max_pos, int rot,
   return KINT_OK;
 }
 
+// How the attention runs (serve_attn.cuh): one launch with a cluster a unit, one cooperative launch, or two launches.
+enum AttnShape : int { SHAPE_CLUSTER = 0, SHAPE_COOP = 1, SHAPE_TWO = 2 };
+
 // Launch shape of the attention, from sizes the host knows.
 struct AttnPlan {
-  int G, nt, tiles, max_slabs, per_split, nsplit, cluster, slab_words, big_words;
+  int G, nt, tiles, max_slabs, slab_words, shape;
+  int blocks, big_words;  // one launch: blocks a unit, floats of shared memory a block keeps scores (then sums) in
+  int per_split, nsplit;  // two launches: slabs a block, blocks a unit
   size_t scores, stats, part, count, bytes;  // byte offsets in the workspace, and its size
 };
-constexpr int kBlocksPerSm = 16 / kAttnWarps;          // of at most 128 registers a thread
-constexpr int kScoreWords = 8192;  // 32 KB of scores a block, beside 20 KB of copies in flight
-constexpr int kBlockSlabs = 32 * kAttnWarps;  // a warp keeps the addresses of 32
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+constexpr int kSms = 152;
+constexpr int kBlocksPerSm = 16 / kAttnWarps;          // of at most 128 registers a thread
+constexpr int kScoreWords = 8192;                      // 32 KB of scores a block, beside 20 KB of copies in flight
+constexpr int kBlockSlabs = 32 * kAttnWarps;           // a warp keeps the addresses of 32
+constexpr int kMinSlabs = 4 * kAttnWarps;              // fewest slabs a block that splitting leaves
 
 bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int sinks, int max_new, int max_len) {
   if (B < 1 || q_heads < 1 || kv < 1 || q_heads % kv || (d != 64 && d != 128) || window < 0 || sinks < 0 || max_new < 1 ||
@@ -84,36 +91,44 @@ bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int s
   a.tiles = (int)tiles;
   a.max_slabs = (int)slabs;
   a.slab_words = rows <= 4 ? 64 : 128 * a.nt;
-  // One launch where a cluster of up to 8 blocks can keep the scores in shared memory, kScoreWords a block (which leaves
-  // room for kBlocksPerSm blocks) or, past what 8 such blocks hold, twice that.  A block costs about 5 us of latency
-  // whatever it does, so a unit is split further only while all blocks still run at once and each has 16 slabs (two a warp).
   const long long most = std::min(kScoreWords / a.slab_words, kBlockSlabs);
-  const long long slots = 152ll * (a.nt == 2 && d == 128 ? kBlocksPerSm / 2 : kBlocksPerSm);
+  const int sums = kAttnWarps * 8 * a.nt * d;
+  // A cluster of up to 8 blocks a unit, 32 KB of scores a block (kBlocksPerSm blocks a SM) or, past what 8 such blocks hold,
+  // 64 KB.  A block costs about 5 us of latency whatever it does, so a unit is split further only while all blocks still
+  // run at once and each has kMinSlabs.
+  const long long slots = (long long)kSms * (a.nt == 2 && d == 128 ? kBlocksPerSm / 2 : kBlocksPerSm);
   int c = (int)std::min<long long>((slabs + most - 1) / most, 8);
-  a.cluster = slabs <= c * std::min<long long>(2 * most, kBlockSlabs);
-  if (a.cluster) {
-    while (2 * c <= 8 && units * c * 2 <= slots && slabs >= 4 * kAttnWarps * c) c *= 2;
-    a.nsplit = c;
-    a.per_split = (int)((slabs + c - 1) / c);
-    a.big_words = std::max(a.per_split * a.slab_words, kAttnWarps * 8 * a.nt * d);
-    a.scores = a.stats = a.part = a.count = 0;
-    a.bytes = 256;  // (unused)
+  a.shape = slabs <= c * std::min<long long>(2 * most, kBlockSlabs) ? SHAPE_CLUSTER : SHAPE_TWO;
+  while (a.shape == SHAPE_CLUSTER && 2 * c <= 8 && units * c * 2 <= slots && slabs >= kMinSlabs * c) c *= 2;
+  // Where the units are so few that twice those blocks and more run at once, a cooperative launch.
+  const long long coop = units > slots ? 0 : std::min(slots / units, (slabs + kMinSlabs - 1) / kMinSlabs);
+  if (coop >= 2 * c && slabs <= coop * most) {
+    a.shape = SHAPE_COOP;
+    c = (int)coop;
+  }
+  a.blocks = c;
+  a.big_words = a.shape == SHAPE_TWO ? 0 : std::max((int)((slabs + c - 1) / c) * a.slab_words, sums);
+  a.scores = a.stats = a.part = a.count = 0;
+  a.per_split = a.nsplit = 0;
+  if (a.shape == SHAPE_CLUSTER) {
+    a.bytes = 256;  // (not touched)
     return units * c <= 0x7fffffffll;
   }
-  // Two launches: 64 slabs a block, fewer while the grid is under two blocks a SM, 8 (one a warp) at least.
+  // Two launches: 64 slabs a block, fewer while the grid is under two blocks a SM, 8 at least.  (A cooperative launch that the
+  // device has no room for runs so too.)
   long long per = 64;
-  while (per > 8 && units * ((slabs + per - 1) / per) < 304) per >>= 1;
+  while (per > 8 && units * ((slabs + per - 1) / per) < 2 * kSms) per >>= 1;
   const long long nsplit = (slabs + per - 1) / per;
   if (units * nsplit > 0x7fffffffll) return false;
   a.per_split = (int)per;
   a.nsplit = (int)nsplit;
-  a.big_words = 0;
+  const size_t parts = (size_t)units * std::max<long long>(nsplit, a.shape == SHAPE_COOP ? c : 0);
   size_t off = 0;
   auto take = [&](size_t n) { const size_t at = off; off = align256(off + n); return at; };
   a.scores = take((size_t)units * slabs * a.slab_words * 4);
-  a.stats = take((size_t)units * nsplit * (a.nt * 16 + 2) * 4);
-  a.part = take((size_t)units * nsplit * a.nt * 8 * (d + 4) * 4);
-  a.count = take((size_t)units * 4);
+  a.stats = take(parts * (a.nt * 16 + 2) * 4);
+  a.part = take(parts * a.nt * 8 * (d + 4) * 4);
+  a.count = take((size_t)units * 2 * 4);
   a.bytes = off;
   return true;
 }
@@ -282,8 +297,8 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
     p.b0l = (float)(-(double)tau * log2e);
     for (int r = 0; r <= Kint; ++r) p.e[r] = (float)std::exp(-(double)tau + r * h);
   }
-  p.G = a.G; p.tiles = a.tiles; p.nt = a.nt; p.nsplit = a.nsplit; p.per_split = a.per_split; p.max_slabs = a.max_slabs;
-  p.slab_words = a.slab_words; p.big_words = a.big_words;
+  p.G = a.G; p.tiles = a.tiles; p.nt = a.nt; p.max_slabs = a.max_slabs; p.slab_words = a.slab_words;
+  p.wait_ns = serve_wait_ns();
   p.by_tiles = fast_div(a.tiles); p.by_kv = fast_div(cache->kv_heads); p.by_G = fast_div(a.G);
   const int vec = 4 * elem_size(dtype);
   p.o_vec = reinterpret_cast<uintptr_t>(out->ptr) % vec == 0 && out->stride_t % 4 == 0 && out->stride_h % 4 == 0;
@@ -291,10 +306,24 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
   p.scores = reinterpret_cast<float*>(ws + a.scores);
   p.stats = reinterpret_cast<float*>(ws + a.stats);
   p.part = reinterpret_cast<float*>(ws + a.part);
-  p.count = reinterpret_cast<int*>(ws + a.count);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   auto launch = [&](int what) { return cache->d == 128 ? launch_attn_128(p, what, s) : launch_attn_64(p, what, s); };
-  if (a.cluster) return traced("k_attn", s, [&] { return launch(ATTN_CLUSTER); });
+  if (a.shape != SHAPE_TWO) {
+    p.nsplit = a.blocks;
+    p.per_split = 0;
+    p.big_words = a.big_words;
+    p.count = nullptr;
+    if (a.shape == SHAPE_CLUSTER) return traced("k_attn", s, [&] { return launch(ATTN_ONE); });
+    p.count = reinterpret_cast<int*>(ws + a.count);
+    const int units = B * cache->kv_heads * a.tiles;
+    if (cudaMemsetAsync(p.count, 0, (size_t)units * 2 * sizeof(int), s) != cudaSuccess) return KINT_ERR_LAUNCH;
+    cudaError_t e = cudaSuccess;
+    rc = traced("k_attn", s, [&] { return e = launch(ATTN_ONE); });
+    if (e != cudaErrorCooperativeLaunchTooLarge) return rc;
+    cudaGetLastError();  // (cleared: the two launches below do the work)
+  }
+  p.nsplit = a.nsplit; p.per_split = a.per_split; p.big_words = 0;
+  p.count = reinterpret_cast<int*>(ws + a.count);
   if ((rc = traced("k_attn_scores", s, [&] { return launch(ATTN_SCORES); }))) return rc;
   return traced("k_attn_values", s, [&] { return launch(ATTN_VALUES); });
 }

@@ -14,8 +14,10 @@
 //   k_attn          one launch: the 1 to 8 blocks of a cluster share a unit (request, kv head, row
 //                   tile), keep their scores in shared memory and exchange extrema and sums through
 //                   distributed shared memory.  Every byte of the cache is read once.
+//                   With few units and long lists, a cooperative launch instead: as many blocks a unit as
+//                   run at once, which exchange through the workspace and wait for one another.
 //   k_attn_scores,  two launches with the scores in the workspace, for lists of keys too long for
-//   k_attn_values   a cluster's shared memory.  The last block of a unit adds the ranges up in order.
+//   k_attn_values   that.  The last block of a unit adds the ranges up in order.
 //
 // Codes go from their load straight to tensor-core operands: the K layout puts the words of
 // one key that a lane feeds to the products next to each other, the V layout the pairs of keys
@@ -182,12 +184,12 @@ __device__ __forceinline__ Share share_of(const AttnP& p, const Unit& u, int i0,
 }
 
 // A warp's ring in shared memory: items (the keys' or the values' part of its slabs: codes and scales, 9 d bytes) arrive by
-// asynchronous 16-byte copies, which hold no registers, two items ahead of the two that are worked on: 18 KB a block are
-// under way.  The keys' items carry the slab's V scales too (their largest sets the unit's power of two).  Only this warp
-// reads its ring, so one warp barrier a pair of items orders everything.
+// asynchronous 16-byte copies, which hold no registers, kStages - 1 items ahead of the work: 14 KB a block are under way.
+// The keys' items carry the slab's V scales too (their largest sets the unit's power of two).  Only this warp
+// reads its ring, so one warp barrier an item orders everything.
 template <int D>
 struct Ring {
-  static constexpr int kAhead = D == 128 ? 2 : 4, kStages = 2 * kAhead, kPlace = 10 * D, kBytes = kWarps * kStages * kPlace;
+  static constexpr int kStages = D == 128 ? 4 : 6, kPlace = 10 * D, kBytes = kWarps * kStages * kPlace;
   uint32_t at;  // shared address of the warp's first place
 
   __device__ __forceinline__ explicit Ring(void* smem) : at(smem_u32(smem) + warp_id_uniform() * kStages * kPlace) {}
@@ -218,29 +220,24 @@ struct Ring {
   __device__ __forceinline__ void prime(const Share& sh) const {
     __syncwarp();
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s)
+    for (int s = 0; s < kStages - 1; ++s) {
       if (s < sh.n) copy<KEYS>(sh, s, s);
-    commit();
+      commit();
+    }
   }
-  // work(l, shared address) for items 0 .. n - 1 in order, kAhead of them between barriers.
+  // work(l, shared address) for items 0 .. n - 1 in order.
   template <bool KEYS, class Work>
   __device__ __forceinline__ void stream(const Share& sh, Work work) const {
     for (int l = 0; l < sh.n; l += kStages) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int m = l + h * kAhead;
-        if (m < sh.n) {
-          asm volatile("cp.async.wait_group 0;" ::: "memory");
-          __syncwarp();  // these items are here for every lane, and the places of those before them have been read
-#pragma unroll
-          for (int s = 0; s < kAhead; ++s)
-            if (m + kAhead + s < sh.n) copy<KEYS>(sh, m + kAhead + s, (1 - h) * kAhead + s);
+      for (int s = 0; s < kStages; ++s)
+        if (l + s < sh.n) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+          __syncwarp();  // item l + s is here for every lane, and the place of the one before it has been read
+          if (l + s + kStages - 1 < sh.n) copy<KEYS>(sh, l + s + kStages - 1, (s + kStages - 1) % kStages);
           commit();
-#pragma unroll
-          for (int s = 0; s < kAhead; ++s)
-            if (s == 0 || m + s < sh.n) work(m + s, at + (h * kAhead + s) * kPlace);
+          work(l + s, at + s * kPlace);
         }
-      }
     }
   }
 };
@@ -652,6 +649,12 @@ __device__ __forceinline__ void split_f16(float2 x, uint32_t& hi, uint32_t& lo) 
   const __half2 l = __float22half2_rn(fma2(r, make_float2(-1.0f, -1.0f), x));
   lo = *reinterpret_cast<const uint32_t*>(&l);
 }
+// The part this lane feeds: hi (take = 0) or lo (take = -1).
+__device__ __forceinline__ uint32_t part_f16(float2 x, float take) {
+  const __half2 h = __float22half2_rn(x);
+  const __half2 y = __float22half2_rn(fma2(__half22float2(h), make_float2(take, take), x));
+  return *reinterpret_cast<const uint32_t*>(&y);
+}
 
 // Sums of the value pass in a thread block's shared memory.
 template <int D, int NT>
@@ -660,25 +663,27 @@ struct Sums {
 };
 
 // Weights of the slabs [i0, i1) and their sums with the values, one partial sum a warp: so[warp][row][D], sums.
-template <int D, int NT, bool F32, int MODE>
+// FOUR: tiles of at most four rows keep the two fp16 parts of a weight in columns r and r + 4 of one product, whose results
+// block_sum adds up; larger tiles take a product for each part.
+template <int D, int NT, bool FOUR, bool F32, int MODE>
 __device__ __forceinline__ void value_pass(const AttnP& p, const Share& sh, const Ring<D>& ring, const float* scores,
                                            const RowMap* maps, const float* tops, const float2* tab, float up, float* so,
                                            Sums<D, NT>& sums, bool alias) {
   constexpr int NG = D / kGroup, R = 8 * NT, MT = D / 16;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const bool four = NT == 1 && p.slab_words == 64;
+  const float take = g < 4 ? 0.0f : -1.0f;
   RowMap rm[NT];
   float top[NT];
   const float2* rt[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int r = four ? g & 3 : 8 * n + g;  // (of four rows, the lanes of the other four repeat them)
+    const int r = FOUR ? g & 3 : 8 * n + g;
     rm[n] = maps[r];
     top[n] = tops[r];
     rt[n] = tab + (p.calib == CAL_MINMAX ? r * table_len(p.Kint) : 0);
   }
   const float eup = (float)((__float_as_int(up) >> 23) - 127);
-  const int in = score_row(four ? g & 3 : g, four);
+  const int in = score_row(FOUR ? g & 3 : g, FOUR);
   float acc[NT][MT][4];
   float2 cs[NT][NG], ws[NT];  // over even and odd keys
 #pragma unroll
@@ -727,8 +732,13 @@ __device__ __forceinline__ void value_pass(const AttnP& p, const Share& sh, cons
           if (w[n][1].x == 0.0f) x1.x = 0.0f; else cs[n][k].x = fmaf(w[n][1].x, c1.x, cs[n][k].x);
           if (w[n][1].y == 0.0f) x1.y = 0.0f; else cs[n][k].y = fmaf(w[n][1].y, c1.y, cs[n][k].y);
         }
-        split_f16(x0, b0[n][0], b0[n][1]);
-        split_f16(x1, b1[n][0], b1[n][1]);
+        if constexpr (FOUR) {
+          b0[n][0] = part_f16(x0, take);
+          b1[n][0] = part_f16(x1, take);
+        } else {
+          split_f16(x0, b0[n][0], b0[n][1]);
+          split_f16(x1, b1[n][0], b1[n][1]);
+        }
       }
 #pragma unroll
       for (int jj = 0; jj < 4; ++jj) {
@@ -738,7 +748,7 @@ __device__ __forceinline__ void value_pass(const AttnP& p, const Share& sh, cons
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int a = 0; a < 2; ++a) mma_f16(acc[n][4 * k + jj], a0, a1, a2, a3, b0[n][a], b1[n][a]);
+          for (int a = 0; a < (FOUR ? 1 : 2); ++a) mma_f16(acc[n][4 * k + jj], a0, a1, a2, a3, b0[n][a], b1[n][a]);
       }
     }
   });
@@ -763,7 +773,7 @@ __device__ __forceinline__ void value_pass(const AttnP& p, const Share& sh, cons
 #pragma unroll
       for (int k = 0; k < NG; ++k) C[k] += __shfl_xor_sync(0xffffffffu, C[k], o);
     }
-    if (t == 0) {
+    if (t == 0 && (!FOUR || g < 4)) {
       sums.w[warp][8 * n + g] = W;
 #pragma unroll
       for (int k = 0; k < NG; ++k) sums.c[warp][8 * n + g][k] = C[k];
@@ -773,7 +783,7 @@ __device__ __forceinline__ void value_pass(const AttnP& p, const Share& sh, cons
 }
 
 // Sums over the block's warps: four channels of row r from channel d on, centres included; the row's weight.
-template <int D, int NT>
+template <int D, int NT, bool FOUR>
 __device__ __forceinline__ float4 block_sum(const float* so, const Sums<D, NT>& s, int r, int d) {
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   float c = 0.0f;
@@ -781,6 +791,10 @@ __device__ __forceinline__ float4 block_sum(const float* so, const Sums<D, NT>& 
   for (int w = 0; w < kWarps; ++w) {
     const float4 x = *reinterpret_cast<const float4*>(so + (w * 8 * NT + r) * D + d);
     o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+    if constexpr (FOUR) {
+      const float4 y = *reinterpret_cast<const float4*>(so + (w * 8 * NT + r + 4) * D + d);
+      o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
+    }
     c += s.c[w][r][d / kGroup];
   }
   return make_float4(o.x + c, o.y + c, o.z + c, o.w + c);
@@ -843,7 +857,62 @@ __device__ __forceinline__ float4 peer_f32x4(uint32_t a) {
   return v;
 }
 
-template <int D, int NT, bool F32, int MODE>
+// All `blocks` blocks of a unit have come here (a cooperative launch: they run at once); what they wrote before is visible.
+// The wait is bounded: past the limit it flags the status word and goes on.
+__device__ __forceinline__ void unit_sync(const AttnP& p, int* counter, int blocks) {
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    atomicAdd(counter, 1);
+    const uint64_t t0 = globaltimer_ns();
+    int seen;
+    while (true) {
+      asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
+      if (seen >= blocks) break;
+      if (globaltimer_ns() - t0 > p.wait_ns) {
+        dev_flag(p.status, DEV_ERR_TIMEOUT_SYNC);
+        break;
+      }
+      __nanosleep(40);
+    }
+  }
+  __syncthreads();
+  __threadfence();
+}
+// The extrema of a unit's `n` ranges, st[range][2 R + 2] (ends with a barrier).
+template <int NT>
+__device__ __forceinline__ void join_extrema(const float* st, int n, BlockExt<NT>& ext) {
+  constexpr int R = 8 * NT;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int r = warp; r <= R; r += kWarps) {  // row R: the V scales
+    float a = r < R ? kMasked : 0.0f, b = INFINITY;
+    for (int s = lane; s < n; s += 32) {
+      const float2 x = __ldcg(reinterpret_cast<const float2*>(st + (size_t)s * (2 * R + 2) + 2 * r));
+      a = max_nan(a, x.x);
+      b = fminf(b, x.y);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
+      b = fminf(b, __shfl_xor_sync(0xffffffffu, b, o));
+    }
+    if (lane == 0) {
+      if (r < R)
+        ext.row[r] = make_float2(a, b);
+      else
+        ext.vs = a;
+    }
+  }
+  __syncthreads();
+}
+template <int NT>
+__device__ __forceinline__ void store_extrema(float* st, const BlockExt<NT>& mine) {
+  constexpr int R = 8 * NT;
+  if (threadIdx.x < R) *reinterpret_cast<float2*>(st + 2 * threadIdx.x) = mine.row[threadIdx.x];
+  if (threadIdx.x == 32) *reinterpret_cast<float2*>(st + 2 * R) = make_float2(mine.vs, 0.0f);
+}
+
+template <int D, int NT, bool FOUR, bool F32, int MODE>
 __global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8 / kWarps)) k_attn(const __grid_constant__ AttnP p) {
   constexpr int R = 8 * NT, V = D / 4;
   extern __shared__ float4 sm4[];
@@ -879,7 +948,12 @@ __global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8
     block_extrema<NT>(e, wext, wvs, mine);
   }
   ring.template prime<false>(sh);
-  if (C > 1) {
+  if (p.count) {
+    float* st = p.stats + (size_t)id * C * (2 * R + 2);
+    store_extrema<NT>(st + (size_t)rank * (2 * R + 2), mine);
+    unit_sync(p, p.count + 2 * id, C);
+    join_extrema<NT>(st, C, ext);
+  } else if (C > 1) {
     cluster_arrive();
     cluster_wait();
     if (threadIdx.x < R) {
@@ -898,18 +972,50 @@ __global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8
     __syncthreads();
   }
   const float up = prepare_rows<NT, MODE>(p, C > 1 ? ext : mine, maps, tops, tab);
-  value_pass<D, NT, F32, MODE>(p, sh, ring, big, maps, tops, tab, up, big, sums, true);
+  value_pass<D, NT, FOUR, F32, MODE>(p, sh, ring, big, maps, tops, tab, up, big, sums, true);
   if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);
   if (C == 1) {
     for (int x = threadIdx.x; x < u.rows * V; x += kThreads) {
       const int r = x / V, d = 4 * (x % V);
-      store_result(p, maps[r], qt.row[r].o + d, block_sum<D, NT>(big, sums, r, d), block_weight<D, NT>(sums, r));
+      store_result(p, maps[r], qt.row[r].o + d, block_sum<D, NT, FOUR>(big, sums, r, d), block_weight<D, NT>(sums, r));
+    }
+    return;
+  }
+  if (p.count) {  // this block's sums into the workspace; then the unit's warps join four channels each, a lane every 32nd block
+    float* all = p.part + (size_t)id * C * (R * (D + 4));
+    float* part = all + (size_t)rank * (R * (D + 4));
+    for (int x = threadIdx.x; x < u.rows * V; x += kThreads) {
+      const int r = x / V, d = 4 * (x % V);
+      *reinterpret_cast<float4*>(part + r * (D + 4) + d) = block_sum<D, NT, FOUR>(big, sums, r, d);
+      if (d == 0) part[r * (D + 4) + D] = block_weight<D, NT>(sums, r);
+    }
+    unit_sync(p, p.count + 2 * id + 1, C);
+    const int lane = threadIdx.x & 31;
+    for (int x = rank * kWarps + warp_id_uniform(); x < u.rows * V; x += C * kWarps) {
+      const int r = x / V, d = 4 * (x % V);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      float W = 0.0f;
+      for (int c = lane; c < C; c += 32) {
+        const float* a = all + (size_t)c * (R * (D + 4)) + r * (D + 4);
+        const float4 y = __ldcg(reinterpret_cast<const float4*>(a + d));
+        o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
+        W += __ldcg(a + D);
+      }
+#pragma unroll
+      for (int k = 16; k; k >>= 1) {
+        o.x += __shfl_xor_sync(0xffffffffu, o.x, k);
+        o.y += __shfl_xor_sync(0xffffffffu, o.y, k);
+        o.z += __shfl_xor_sync(0xffffffffu, o.z, k);
+        o.w += __shfl_xor_sync(0xffffffffu, o.w, k);
+        W += __shfl_xor_sync(0xffffffffu, W, k);
+      }
+      if (lane == 0) store_result(p, maps[r], qt.row[r].o + d, o, W);
     }
     return;
   }
   // this block's sums over its own warps, in place of warp 0's; then each block of the cluster joins its share of them
   for (int x = threadIdx.x; x < u.rows * V; x += kThreads)
-    *reinterpret_cast<float4*>(big + 4 * x) = block_sum<D, NT>(big, sums, x / V, 4 * (x % V));
+    *reinterpret_cast<float4*>(big + 4 * x) = block_sum<D, NT, FOUR>(big, sums, x / V, 4 * (x % V));
   if (threadIdx.x < R) bw[threadIdx.x] = block_weight<D, NT>(sums, threadIdx.x);
   cluster_arrive();
   cluster_wait();
@@ -957,14 +1063,12 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attn_scores(const __g
     Extrema<NT> e;
     key_pass<D, NT, F32, LOW>(p, u, qt, sh, ring, i0, p.scores + ((size_t)id * p.max_slabs + i0) * p.slab_words, e);
     block_extrema<NT>(e, wext, wvs, mine);
-    float* st = p.stats + ((size_t)id * p.nsplit + split) * (2 * R + 2);
-    if (threadIdx.x < R) *reinterpret_cast<float2*>(st + 2 * threadIdx.x) = mine.row[threadIdx.x];
-    if (threadIdx.x == 32) *reinterpret_cast<float2*>(st + 2 * R) = make_float2(mine.vs, 0.0f);
+    store_extrema<NT>(p.stats + ((size_t)id * p.nsplit + split) * (2 * R + 2), mine);
   }
   if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);
 }
 
-template <int D, int NT, bool F32, int MODE>
+template <int D, int NT, bool FOUR, bool F32, int MODE>
 __global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8 / kWarps)) k_attn_values(const __grid_constant__ AttnP p) {
   constexpr int R = 8 * NT, V = D / 4;
   extern __shared__ float4 sm4[];
@@ -992,35 +1096,14 @@ __global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8
   const Share sh = share_of(p, u, i0, i1, addr, bad);
   const Ring<D> ring(sm4);
   ring.template prime<false>(sh);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const float* st = p.stats + (size_t)id * p.nsplit * (2 * R + 2);
-  for (int r = warp; r <= R; r += kWarps) {  // row R: the V scales
-    float a = r < R ? kMasked : 0.0f, b = INFINITY;
-    for (int s = lane; s < active; s += 32) {
-      const float2 x = *reinterpret_cast<const float2*>(st + (size_t)s * (2 * R + 2) + 2 * r);
-      a = max_nan(a, x.x);
-      b = fminf(b, x.y);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
-      b = fminf(b, __shfl_xor_sync(0xffffffffu, b, o));
-    }
-    if (lane == 0) {
-      if (r < R)
-        ext.row[r] = make_float2(a, b);
-      else
-        ext.vs = a;
-    }
-  }
-  __syncthreads();
+  join_extrema<NT>(p.stats + (size_t)id * p.nsplit * (2 * R + 2), active, ext);
   const float up = prepare_rows<NT, MODE>(p, ext, maps, tops, tab);
-  value_pass<D, NT, F32, MODE>(p, sh, ring, p.scores + ((size_t)id * p.max_slabs + i0) * p.slab_words, maps, tops, tab, up, so, sums,
+  value_pass<D, NT, FOUR, F32, MODE>(p, sh, ring, p.scores + ((size_t)id * p.max_slabs + i0) * p.slab_words, maps, tops, tab, up, so, sums,
                                false);
   float* part = p.part + ((size_t)id * p.nsplit + split) * (R * (D + 4));
   for (int x = threadIdx.x; x < u.rows * V; x += kThreads) {
     const int r = x / V, d = 4 * (x % V);
-    const float4 o = block_sum<D, NT>(so, sums, r, d);
+    const float4 o = block_sum<D, NT, FOUR>(so, sums, r, d);
     const float W = block_weight<D, NT>(sums, r);
     if (active == 1) {
       store_result(p, maps[r], row_of(p, u, r).o + d, o, W);
@@ -1084,19 +1167,20 @@ cudaError_t want_smem(Kern kern, int bytes, std::atomic<int> (&granted)[kMaxGran
   return e;
 }
 
-template <int D, int NT, bool F32, int MODE>
+template <int D, int NT, bool FOUR, bool F32, int MODE>
 cudaError_t go(const AttnP& p, int what, int grid, cudaStream_t s) {
   const int tab = MODE == M_GRID ? (p.calib == CAL_MINMAX ? 8 * NT : 1) * table_len(p.Kint) * (int)sizeof(float2) : 0;
-  if (what == ATTN_CLUSTER) {
+  if (what == ATTN_ONE) {
     const int smem = Ring<D>::kBytes + p.big_words * 4 + tab;
     static std::atomic<int> granted[kMaxGranted];
-    if (cudaError_t e = want_smem(k_attn<D, NT, F32, MODE>, smem, granted)) return e;
-    return launch_pdl_cluster(k_attn<D, NT, F32, MODE>, dim3(grid), dim3(kThreads), smem, p.nsplit, s, p);
+    if (cudaError_t e = want_smem(k_attn<D, NT, FOUR, F32, MODE>, smem, granted)) return e;
+    if (p.count) return launch_cooperative(k_attn<D, NT, FOUR, F32, MODE>, dim3(grid), dim3(kThreads), smem, s, p);
+    return launch_pdl_cluster(k_attn<D, NT, FOUR, F32, MODE>, dim3(grid), dim3(kThreads), smem, p.nsplit, s, p);
   }
   const int smem = Ring<D>::kBytes + kWarps * 8 * NT * D * (int)sizeof(float) + tab;
   static std::atomic<int> granted[kMaxGranted];
-  if (cudaError_t e = want_smem(k_attn_values<D, NT, F32, MODE>, smem, granted)) return e;
-  return launch_pdl(k_attn_values<D, NT, F32, MODE>, dim3(grid), dim3(kThreads), smem, s, p);
+  if (cudaError_t e = want_smem(k_attn_values<D, NT, FOUR, F32, MODE>, smem, granted)) return e;
+  return launch_pdl(k_attn_values<D, NT, FOUR, F32, MODE>, dim3(grid), dim3(kThreads), smem, s, p);
 }
 template <int D, int NT, bool F32, bool LOW>
 cudaError_t go_scores(const AttnP& p, int grid, cudaStream_t s) {
@@ -1105,21 +1189,29 @@ cudaError_t go_scores(const AttnP& p, int grid, cudaStream_t s) {
   if (cudaError_t e = want_smem(k_attn_scores<D, NT, F32, LOW>, smem, granted)) return e;
   return launch_pdl(k_attn_scores<D, NT, F32, LOW>, dim3(grid), dim3(kThreads), smem, s, p);
 }
-template <int D, int NT, bool F32>
+template <int D, int NT, bool FOUR, bool F32>
 cudaError_t pick_mode(const AttnP& p, int what, int grid, cudaStream_t s) {
-  if (what == ATTN_SCORES) return p.calib == CAL_MINMAX ? go_scores<D, NT, F32, true>(p, grid, s) : go_scores<D, NT, F32, false>(p, grid, s);
   switch (p.calib) {
-    case CAL_SOFTMAX: return go<D, NT, F32, M_EXP>(p, what, grid, s);
+    case CAL_SOFTMAX: return go<D, NT, FOUR, F32, M_EXP>(p, what, grid, s);
     case CAL_FWM:
-    case CAL_MINMAX: return go<D, NT, F32, M_GRID>(p, what, grid, s);
-    default: return go<D, NT, F32, M_RARE>(p, what, grid, s);
+    case CAL_MINMAX: return go<D, NT, FOUR, F32, M_GRID>(p, what, grid, s);
+    default: return go<D, NT, FOUR, F32, M_RARE>(p, what, grid, s);
   }
+}
+template <int D, bool F32>
+cudaError_t pick_rows(const AttnP& p, int what, cudaStream_t s) {
+  const int grid = p.B * p.c.kv * p.tiles * p.nsplit;
+  const bool low = p.calib == CAL_MINMAX;
+  if (what == ATTN_SCORES) {
+    if (p.nt == 1) return low ? go_scores<D, 1, F32, true>(p, grid, s) : go_scores<D, 1, F32, false>(p, grid, s);
+    return low ? go_scores<D, 2, F32, true>(p, grid, s) : go_scores<D, 2, F32, false>(p, grid, s);
+  }
+  if (p.slab_words == 64) return pick_mode<D, 1, true, F32>(p, what, grid, s);
+  return p.nt == 1 ? pick_mode<D, 1, false, F32>(p, what, grid, s) : pick_mode<D, 2, false, F32>(p, what, grid, s);
 }
 template <int D>
 cudaError_t pick(const AttnP& p, int what, cudaStream_t s) {
-  const int grid = p.B * p.c.kv * p.tiles * p.nsplit;
-  if (p.dtype == DT_FP32) return p.nt == 1 ? pick_mode<D, 1, true>(p, what, grid, s) : pick_mode<D, 2, true>(p, what, grid, s);
-  return p.nt == 1 ? pick_mode<D, 1, false>(p, what, grid, s) : pick_mode<D, 2, false>(p, what, grid, s);
+  return p.dtype == DT_FP32 ? pick_rows<D, true>(p, what, s) : pick_rows<D, false>(p, what, s);
 }
 
 }  // namespace

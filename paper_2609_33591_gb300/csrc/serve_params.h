@@ -94,7 +94,8 @@ struct AttnP {
   float* scores;                     // [unit][max_slabs][slab_words]
   float* stats;                      // [unit][nsplit][nt * 16 + 2]: extrema of each row, the largest V scale
   float* part;                       // [unit][nsplit][nt * 8][d + 1]
-  int* count;                        // [unit]
+  int* count;                        // one cooperative launch: [unit][2], zero before it; two launches: [unit]
+  unsigned long long wait_ns;        // limit of a wait for the other blocks
   FastDiv by_tiles, by_kv, by_G;
   int o_vec;                         // four channels of the output in one access
   unsigned* status;
@@ -105,9 +106,25 @@ cudaError_t launch_rope_table(const RopeTableP& p, cudaStream_t s);
 cudaError_t launch_rope(const RopeP& p, int nsm, cudaStream_t s);
 cudaError_t launch_append(CacheIoP p, int nsm, cudaStream_t s);
 cudaError_t launch_read(CacheIoP p, int nsm, cudaStream_t s);
-enum AttnKernel : int { ATTN_CLUSTER = 0, ATTN_SCORES = 1, ATTN_VALUES = 2 };
+enum AttnKernel : int { ATTN_ONE = 0, ATTN_SCORES = 1, ATTN_VALUES = 2 };
 cudaError_t launch_attn_64(const AttnP& p, int what, cudaStream_t s);
 cudaError_t launch_attn_128(const AttnP& p, int what, cudaStream_t s);
+
+// A launch whose blocks all run at once (or that the runtime refuses).
+template <class Kern, class... Args>
+cudaError_t launch_cooperative(Kern kern, dim3 grid, dim3 block, int smem, cudaStream_t s, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
 
 // launch_pdl with thread-block clusters of `cluster` blocks.
 template <class Kern, class... Args>
@@ -131,6 +148,7 @@ cudaError_t launch_pdl_cluster(Kern kern, dim3 grid, dim3 block, int smem, int c
 // From kint_api.cu: the status word of the current device (checks it once), its SM count, and the launch hook.
 int serve_device(unsigned** status);
 int serve_num_sms();
+unsigned long long serve_wait_ns();
 void serve_hook(const char* kernel, int phase, cudaStream_t s);
 
 }  // namespace kint

@@ -133,6 +133,18 @@ def test_long_context_joined_from_many_parts(calib, dtype):
     check_attention([9001, 40], [1, 1], 4, 1, 64, kint.Config(Kint=16, calib=calib, tau=8.0), dtype, block=128, seed=8, scale=2.0)
 
 
+@pytest.mark.parametrize("heads,new,d", [(2, 1, 128), (8, 1, 64), (16, 1, 128), (5, 3, 64)])
+def test_few_units_with_long_lists(heads, new, d):
+    """One request on many thread blocks at once (a cooperative launch): tiles of 4, 8 and 16 rows, an empty request beside it."""
+    cfg = kint.Config(Kint=8, calib=MM, recon=LERP)
+    check_attention([4100, 0, 3], [new, 0, min(new, 3)], heads, 1, d, cfg, F32, block=64, seed=15)
+
+
+def test_many_tiles_with_long_lists():
+    """Scores too many for shared memory: two launches, joined by the last block of each tile."""
+    check_attention([8500], [150], 16, 1, 64, kint.Config(calib=SOFT), F32, block=256, seed=16)
+
+
 def test_rows_that_see_nothing_are_zero():
     """More new tokens than cached ones (the first rows lie before position 0), and an empty request between others."""
     cfg = kint.Config(Kint=4, calib=MM)
