@@ -73,7 +73,7 @@ constexpr int kSms = 152;
 constexpr int kBlocksPerSm = 16 / kAttnWarps;          // of at most 128 registers a thread
 constexpr int kScoreWords = 8192;                      // 32 KB of scores a block, beside 20 KB of copies in flight
 constexpr int kBlockSlabs = 32 * kAttnWarps;           // a warp keeps the addresses of 32
-constexpr int kMinSlabs = 4 * kAttnWarps;              // fewest slabs a block that splitting leaves
+constexpr int kMinSlabs = 8 * kAttnWarps;              // fewest slabs a block that splitting leaves
 
 bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int sinks, int max_new, int max_len) {
   if (B < 1 || q_heads < 1 || kv < 1 || q_heads % kv || (d != 64 && d != 128) || window < 0 || sinks < 0 || max_new < 1 ||
@@ -96,7 +96,7 @@ bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int s
   // A cluster of up to 8 blocks a unit, 32 KB of scores a block (kBlocksPerSm blocks a SM) or, past what 8 such blocks hold,
   // 64 KB.  A block costs about 5 us of latency whatever it does, so a unit is split further only while all blocks still
   // run at once and each has kMinSlabs.
-  const long long slots = (long long)kSms * (a.nt == 2 && d == 128 ? kBlocksPerSm / 2 : kBlocksPerSm);
+  const long long slots = (long long)kSms * (a.nt == 2 && d == 128 ? 3 * kBlocksPerSm / 4 : kBlocksPerSm);
   int c = (int)std::min<long long>((slabs + most - 1) / most, 8);
   a.shape = slabs <= c * std::min<long long>(2 * most, kBlockSlabs) ? SHAPE_CLUSTER : SHAPE_TWO;
   while (a.shape == SHAPE_CLUSTER && 2 * c <= 8 && units * c * 2 <= slots && slabs >= kMinSlabs * c) c *= 2;

@@ -851,6 +851,12 @@ __device__ __forceinline__ float peer_f32(uint32_t a) {
   return v;
 }
 
+constexpr int kMaxCluster = 8;
+__device__ __forceinline__ float2 peer_f32x2(uint32_t a) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+  return v;
+}
 __device__ __forceinline__ float4 peer_f32x4(uint32_t a) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
@@ -913,7 +919,7 @@ __device__ __forceinline__ void store_extrema(float* st, const BlockExt<NT>& min
 }
 
 template <int D, int NT, bool FOUR, bool F32, int MODE>
-__global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8 / kWarps)) k_attn(const __grid_constant__ AttnP p) {
+__global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps : 16 / kWarps) k_attn(const __grid_constant__ AttnP p) {
   constexpr int R = 8 * NT, V = D / 4;
   extern __shared__ float4 sm4[];
   float* big = reinterpret_cast<float*>(sm4) + Ring<D>::kBytes / 4;  // scores [chunk][slab_words], then partial sums [kWarps][R][D]
@@ -957,17 +963,22 @@ __global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8
     cluster_arrive();
     cluster_wait();
     if (threadIdx.x < R) {
+      float2 x[kMaxCluster];  // (all loads first)
+#pragma unroll
+      for (int c = 0; c < kMaxCluster; ++c) x[c] = c < C ? peer_f32x2(peer(&mine.row[threadIdx.x], c)) : make_float2(kMasked, INFINITY);
       float a = kMasked, b = INFINITY;
-      for (int c = 0; c < C; ++c) {
-        const uint32_t at = peer(&mine.row[threadIdx.x], c);
-        a = max_nan(a, peer_f32(at));
-        b = fminf(b, peer_f32(at + 4));
+#pragma unroll
+      for (int c = 0; c < kMaxCluster; ++c) {
+        a = max_nan(a, x[c].x);
+        b = fminf(b, x[c].y);
       }
       ext.row[threadIdx.x] = make_float2(a, b);
-    } else if (threadIdx.x == 32) {
-      float v = 0.0f;
-      for (int c = 0; c < C; ++c) v = fmaxf(v, peer_f32(peer(&mine.vs, c)));
-      ext.vs = v;
+    } else if (threadIdx.x >= 32 && threadIdx.x < 64) {
+      const int c = threadIdx.x - 32;
+      float v = c < C ? peer_f32(peer(&mine.vs, c)) : 0.0f;
+#pragma unroll
+      for (int o = kMaxCluster / 2; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+      if (c == 0) ext.vs = v;
     }
     __syncthreads();
   }
@@ -1021,12 +1032,17 @@ __global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8
   cluster_wait();
   for (int x = rank + C * threadIdx.x; x < u.rows * V; x += C * kThreads) {
     const int r = x / V;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float W = 0.0f;
-    for (int c = 0; c < C; ++c) {
-      const float4 y = peer_f32x4(peer(big + 4 * x, c));
-      o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
-      W += peer_f32(peer(bw + r, c));
+    float4 y[kMaxCluster], o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float w[kMaxCluster], W = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kMaxCluster; ++c) {
+      y[c] = c < C ? peer_f32x4(peer(big + 4 * x, c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      w[c] = c < C ? peer_f32(peer(bw + r, c)) : 0.0f;
+    }
+#pragma unroll
+    for (int c = 0; c < kMaxCluster; ++c) {
+      o.x += y[c].x; o.y += y[c].y; o.z += y[c].z; o.w += y[c].w;
+      W += w[c];
     }
     store_result(p, maps[r], qt.row[r].o + 4 * (x % V), o, W);
   }
@@ -1069,7 +1085,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attn_scores(const __g
 }
 
 template <int D, int NT, bool FOUR, bool F32, int MODE>
-__global__ void __launch_bounds__(kThreads, ((NT == 2 && D == 128) ? 1 : 2) * (8 / kWarps)) k_attn_values(const __grid_constant__ AttnP p) {
+__global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps : 16 / kWarps) k_attn_values(const __grid_constant__ AttnP p) {
   constexpr int R = 8 * NT, V = D / 4;
   extern __shared__ float4 sm4[];
   float* so = reinterpret_cast<float*>(sm4) + Ring<D>::kBytes / 4;  // [kWarps][R][D]
