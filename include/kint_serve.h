@@ -128,21 +128,22 @@ int kint_cache_read(const kint_cache* cache, const int64_t* slots, int tokens, c
  *   q, out   [rows][q_heads][d] (stride_b unused); q_heads a multiple of kv_heads (consecutive query heads share one)
  *   table    [B][table_stride] int32 block numbers, `width` of a row used
  *   lens     [B] int32: cached tokens, the new ones among them
- *   cu       [B + 1] int32: request b's new tokens are rows cu[b] .. cu[b + 1] - 1, its last positions:
- *            row r sits at position p = lens[b] - cu[b + 1] + r
+ *   cu       [B + 1] int32: request b's new tokens are rows cu[b] .. cu[b + 1] - 1 of the `rows` there are, its last
+ *            positions: row r sits at position p = lens[b] - cu[b + 1] + r
  *   A row sees keys j <= p, and with window > 0 only those with j > p - window or j < sinks.  A row that sees no key
  *   (p < 0) gives zeros.
  *   Kint, calib, tau, recon: the weights, as for kint_attn_fwd (the hard forward under Nearest); the grid is
  *   anchored at the row's extrema over the keys it sees.
  *   max_new  bound on cu[b + 1] - cu[b]; max_len bound on lens[b] (<= width * block_size): they size the launch and
- *            the workspace; rows or keys past them are left out and flagged.
+ *            the workspace; rows or keys past them are left out and flagged, and so are requests whose rows do not lie
+ *            within 0 .. rows.
  *   workspace: kint_cache_attn_workspace_bytes bytes (16-byte aligned).  256 bytes are asked for, and not touched, where the
  *            scores fit the shared memory of one launch.
  * Results do not depend on the order in which thread blocks run.
  */
 int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache* cache, const int32_t* table,
-                    int table_stride, int width, const int32_t* lens, const int32_t* cu, int B, int window, int sinks,
-                    int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
+                    int table_stride, int width, const int32_t* lens, const int32_t* cu, int rows, int B, int window,
+                    int sinks, int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
                     void* workspace, size_t workspace_bytes, void* stream);
 size_t kint_cache_attn_workspace_bytes(int B, int q_heads, int kv_heads, int d, int window, int sinks, int max_new,
                                        int max_len);

@@ -260,8 +260,8 @@ size_t kint_cache_attn_workspace_bytes(int B, int q_heads, int kv_heads, int d, 
 }
 
 int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache* cache, const int32_t* table,
-                    int table_stride, int width, const int32_t* lens, const int32_t* cu, int B, int window, int sinks,
-                    int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
+                    int table_stride, int width, const int32_t* lens, const int32_t* cu, int rows, int B, int window,
+                    int sinks, int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
                     void* workspace, size_t workspace_bytes, void* stream) {
   if (!valid_dtype(dtype) || !table || !lens || !cu || B < 1 || width < 1 || table_stride < width) return KINT_ERR_ARG;
   if (calib < 0 || calib > 5 || recon < 0 || recon > 1) return KINT_ERR_ARG;
@@ -272,7 +272,7 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
   if (rc) return rc;
   if ((rc = check_heads(q, dtype)) || (rc = check_heads(out, dtype))) return rc;
   if (q->heads < 1 || q->heads != out->heads || q->heads % cache->kv_heads) return KINT_ERR_ARG;
-  if (window < 0 || sinks < 0 || max_new < 1 || max_len < 1) return KINT_ERR_ARG;
+  if (rows < 0 || window < 0 || sinks < 0 || max_new < 1 || max_len < 1) return KINT_ERR_ARG;
   if ((long long)max_len > (long long)width * cache->block_size) return KINT_ERR_ARG;
   if (max_len > (1 << 30) || max_new > (1 << 24) || q->heads > (1 << 16)) return KINT_ERR_UNSUPPORTED;
   for (const void* x : {(const void*)table, (const void*)lens, (const void*)cu})
@@ -285,7 +285,7 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
   if ((rc = serve_device(&p.status))) return rc;
   p.q = heads_of(q); p.o = heads_of(out); p.c = cache_of(cache);
   p.table = table; p.lens = lens; p.cu = cu; p.table_stride = table_stride; p.width = width;
-  p.B = B; p.window = std::min(window, 1 << 30); p.sinks = std::min(sinks, 1 << 30); p.max_new = max_new; p.max_len = max_len;
+  p.rows = rows; p.B = B; p.window = std::min(window, 1 << 30); p.sinks = std::min(sinks, 1 << 30); p.max_new = max_new; p.max_len = max_len;
   p.Kint = grid ? Kint : 1; p.calib = calib; p.recon = recon; p.dtype = dtype;
   p.tau = tau; p.scale = (float)(1.0 / std::sqrt((double)cache->d));
   p.inv_h = p.hl = p.b0l = 0.0f;

@@ -83,7 +83,7 @@ struct AttnP {
   Cache c;
   const int32_t *table, *lens, *cu;
   int table_stride, width;
-  int B, window, sinks, max_new, max_len;
+  int rows, B, window, sinks, max_new, max_len;
   int Kint, calib, recon, dtype;
   float tau, scale, inv_h, hl, b0l;  // inv_h = K / tau; hl, b0l: the resolved grid below the window
   float e[KMAX + 2];                 // FWM grid values

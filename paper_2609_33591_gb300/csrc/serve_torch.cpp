@@ -332,7 +332,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         ws = tensor(a[14], "ws");
         need(ws.is_cuda() && ws.is_contiguous(), "ws: expected a contiguous CUDA tensor");
       }
-      run(api.attn(&hq, &ho, &c, pt, (int)table.stride(0), width, pl, pc, B, window, sinks, whole(a[5]), (kint_calib)whole(a[6]),
+      run(api.attn(&hq, &ho, &c, pt, (int)table.stride(0), width, pl, pc, (int)q.size(0), B, window, sinks, whole(a[5]), (kint_calib)whole(a[6]),
                    (float)tau, (kint_recon)whole(a[8]), max_new, max_len, type_of(q, "q"), ws.data_ptr(), ws.is_same(pages) ? kUnusedWorkspace : ws.nbytes(),
                    stream_of(a[15])),
           "kint_cache_attn");

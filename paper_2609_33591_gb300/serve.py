@@ -61,7 +61,7 @@ def load():
                 ("kint_rope", [hp, hp, hp, hp, vp, ll, vp, i, i, i, i, i, i, i, i, vp], i),
                 ("kint_cache_append", [cp, hp, hp, vp, i, hp, hp, vp, vp, i, i, i, i, vp], i),
                 ("kint_cache_read", [cp, vp, i, hp, hp, i, vp], i),
-                ("kint_cache_attn", [hp, hp, cp, vp, i, i, vp, vp, i, i, i, i, i, f, i, i, i, i, vp, sz, vp], i),
+                ("kint_cache_attn", [hp, hp, cp, vp, i, i, vp, vp, i, i, i, i, i, i, f, i, i, i, i, vp, sz, vp], i),
                 ("kint_cache_attn_workspace_bytes", [i] * 8, sz)):
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, res

@@ -270,6 +270,11 @@ def test_index_data_out_of_range_is_flagged_not_followed():
         expect_flag()
     serve.attention(q, pages, gpu(pool.table), ints([70]), ints([0, 1]), cfg)  # a length past the table
     expect_flag()
+    for cu in ([-1, 0], [0, 2], [1, 2], [3, 2]):  # rows that q does not have
+        out = torch.full_like(q, 7.0)
+        serve.attention(q, pages, gpu(pool.table), gpu(pool.lens), ints(cu), cfg, max_new=4, out=out)
+        expect_flag()
+        assert (out == 7.0).all()
     before = pages.clone()
     x = torch.randn(3, 2, 64, device="cuda")
     serve.append(x, x, ints([-1, -2, pages.size(0) * 32], torch.int64), pages)

@@ -34,14 +34,14 @@ def cache(**kw):
     return serve.kint_cache(*a.values())
 
 
-ATTN = dict(q=heads(), out=heads(), cache=cache(), table=P, stride=8, width=8, lens=P, cu=P, B=2, window=0, sinks=0, Kint=4,
+ATTN = dict(q=heads(), out=heads(), cache=cache(), table=P, stride=8, width=8, lens=P, cu=P, rows=2, B=2, window=0, sinks=0, Kint=4,
             calib=1, tau=8.0, recon=0, max_new=1, max_len=256, dtype=0, ws=P, bytes=1 << 40, stream=None)
 
 
 @pytest.mark.parametrize("kw,code", [
     (dict(B=0), -1), (dict(table=None), -1), (dict(stride=7), -1), (dict(width=0), -1), (dict(Kint=0), -1), (dict(Kint=65), -1),
     (dict(tau=0.0), -1), (dict(tau=math.inf), -1), (dict(calib=6), -1), (dict(recon=2), -1), (dict(dtype=3), -1),
-    (dict(window=-1), -1), (dict(sinks=-1), -1), (dict(max_new=0), -1), (dict(max_len=0), -1), (dict(max_len=257), -1),
+    (dict(window=-1), -1), (dict(sinks=-1), -1), (dict(max_new=0), -1), (dict(rows=-1), -1), (dict(max_len=0), -1), (dict(max_len=257), -1),
     (dict(q=heads(6), out=heads(6)), -1), (dict(out=heads(8)), -1), (dict(q=heads(ptr=None)), -1), (dict(q=heads(ptr=P + 2)), -3),
     (dict(lens=P + 2), -3), (dict(cache=cache(d=96)), -2), (dict(cache=cache(block_size=48)), -2), (dict(cache=cache(block_size=8)), -2),
     (dict(cache=cache(num_blocks=0)), -1), (dict(cache=cache(block_stride=9200)), -1), (dict(cache=cache(block_stride=9224)), -3),
