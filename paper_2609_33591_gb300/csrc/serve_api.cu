@@ -300,7 +300,8 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
   p.G = a.G; p.tiles = a.tiles; p.nt = a.nt; p.max_slabs = a.max_slabs; p.slab_words = a.slab_words;
   p.wait_ns = serve_wait_ns();
   p.by_tiles = fast_div(a.tiles); p.by_kv = fast_div(cache->kv_heads); p.by_G = fast_div(a.G);
-  const int vec = 4 * elem_size(dtype);
+  const int vec = 4 * elem_size(dtype), qn = cache->d / 32, qvec = qn * elem_size(dtype);
+  p.q_vec = reinterpret_cast<uintptr_t>(q->ptr) % qvec == 0 && q->stride_t % qn == 0 && q->stride_h % qn == 0;
   p.o_vec = reinterpret_cast<uintptr_t>(out->ptr) % vec == 0 && out->stride_t % 4 == 0 && out->stride_h % 4 == 0;
   char* ws = static_cast<char*>(workspace);
   p.scores = reinterpret_cast<float*>(ws + a.scores);

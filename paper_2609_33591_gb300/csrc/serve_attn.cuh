@@ -294,10 +294,15 @@ __device__ __forceinline__ int score_row(int r, bool four) {  // with the bit th
 }
 __device__ __forceinline__ int score_at(int row, int key) { return (row & ~8) + (key ^ (row & 8)); }
 
-__device__ __forceinline__ float load_q(const AttnP& p, long long off) {
-  if (p.dtype == DT_FP32) return static_cast<const float*>(p.q.p)[off];
-  if (p.dtype == DT_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p.q.p)[off]);
-  return __half2float(static_cast<const __half*>(p.q.p)[off]);
+// N consecutive channels of a query row.
+template <int N, bool F32>
+__device__ __forceinline__ void load_q(const AttnP& p, long long off, float (&x)[N]) {
+  if constexpr (F32)
+    load_ch<float, N>(static_cast<const float*>(p.q.p) + off, p.q_vec, x);
+  else if (p.dtype == DT_BF16)
+    load_ch<__nv_bfloat16, N>(static_cast<const __nv_bfloat16*>(p.q.p) + off, p.q_vec, x);
+  else
+    load_ch<__half, N>(static_cast<const __half*>(p.q.p) + off, p.q_vec, x);
 }
 // Four consecutive channels of the output.
 __device__ __forceinline__ void store_o(const AttnP& p, long long off, const float (&x)[4]) {
@@ -338,46 +343,61 @@ struct QTile {
   Row row[8 * NT];
 };
 
+// A warp's query rows (every kWarps-th) in registers: loaded before the tables and the first slabs are waited for.
 template <int D, int NT, bool F32>
-__device__ __forceinline__ void load_qtile(const AttnP& p, const Unit& u, QTile<D, NT, F32>& t, __half (*part)[8 * NT][D + 8]) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  constexpr int N = D / 32;
-  for (int r = warp; r < 8 * NT; r += kWarps) {
-    const Row row = row_of(p, u, r);
-    float x[N];
-    float top = 0.0f;
+struct QRegs {
+  static constexpr int N = D / 32, kRows = 8 * NT / kWarps;
+  float x[kRows][N];
+  Row row[kRows];
+
+  __device__ __forceinline__ void load(const AttnP& p, const Unit& u) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      x[i] = r < u.rows ? load_q(p, row.q + lane * N + i) : 0.0f;
-      top = fmaxf(top, fabsf(x[i]));
-    }
+    for (int k = 0; k < kRows; ++k) {
+      const int r = warp + k * kWarps;
+      row[k] = row_of(p, u, r);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    // k = exponent of top - 13 (top finite and not 0; a subnormal maximum counts as a small normal one)
-    const int ex = (top > 0.0f && top < __int_as_float(0x7f800000)) ? max((__float_as_int(top) >> 23) - 127, -90) - 13 : 0;
-    const float down = __int_as_float((127 - ex) << 23), up = __int_as_float((127 + ex) << 23);
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int ch = lane * N + i;
-      float y = x[i] * down;
-      s += y;
-      if (!F32 && (ch & 1)) y *= 0.0625f;  // odd nibbles sit at bits 4
-      const __half hi = __float2half_rn(y);
-      part[0][r][ch] = hi;
-      if constexpr (F32) part[1][r][ch] = __float2half_rn(y - __half2float(hi));
-    }
-    // 16 * 4 (d = 128) or 32 * 2 (d = 64) channels a group
-#pragma unroll
-    for (int o = kGroup / N / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (!F32) s *= 1.0f / kCodeUnit;
-    if (lane % (kGroup / N) == 0) t.sum[r][lane * N / kGroup] = s;
-    if (lane == 0) {
-      t.mul[r] = up * p.scale * (F32 ? 1.0f : kCodeUnit);
-      t.row[r] = row;
+      for (int i = 0; i < N; ++i) x[k][i] = 0.0f;
+      if (r < u.rows) load_q<N, F32>(p, row[k].q + lane * N, x[k]);
     }
   }
-}
+  __device__ __forceinline__ void store(const AttnP& p, QTile<D, NT, F32>& t, __half (*part)[8 * NT][D + 8]) const {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) t.part = part;
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const int r = warp + k * kWarps;
+      float top = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(x[k][i]));
+#pragma unroll
+      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      // 2^ex = exponent of top - 13 (top finite and not 0; a subnormal maximum counts as a small normal one)
+      const int ex = (top > 0.0f && top < __int_as_float(0x7f800000)) ? max((__float_as_int(top) >> 23) - 127, -90) - 13 : 0;
+      const float down = __int_as_float((127 - ex) << 23), up = __int_as_float((127 + ex) << 23);
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int ch = lane * N + i;
+        float y = x[k][i] * down;
+        s += y;
+        if (!F32 && (ch & 1)) y *= 0.0625f;  // odd nibbles sit at bits 4
+        const __half hi = __float2half_rn(y);
+        part[0][r][ch] = hi;
+        if constexpr (F32) part[1][r][ch] = __float2half_rn(y - __half2float(hi));
+      }
+      // 16 * 4 (d = 128) or 32 * 2 (d = 64) channels a group
+#pragma unroll
+      for (int o = kGroup / N / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if (!F32) s *= 1.0f / kCodeUnit;
+      if (lane % (kGroup / N) == 0) t.sum[r][lane * N / kGroup] = s;
+      if (lane == 0) {
+        t.mul[r] = up * p.scale * (F32 ? 1.0f : kCodeUnit);
+        t.row[r] = row[k];
+      }
+    }
+  }
+};
 
 // What the key pass leaves besides the scores: per row the largest (NaN where a score is) and smallest score, and the largest V scale.
 template <int NT>
@@ -584,8 +604,9 @@ __device__ __forceinline__ RowMap row_map(const AttnP& p, float M, float m, floa
   return r;
 }
 
-// The half-bin table of one row (MinMax) or of all (FWM), filled by `n` threads.
-__device__ __forceinline__ void fill_table(const AttnP& p, float2* tab, float span, bool flat, float up, int at, int n) {
+// The half-bin table of one row (MinMax) or of all (FWM, from its grid values in shared memory: the parameters answer one
+// address a time), filled by `n` threads.
+__device__ __forceinline__ void fill_table(const AttnP& p, float2* tab, const float* grid, float span, bool flat, float up, int at, int n) {
   const bool mm = p.calib == CAL_MINMAX;
   const float h = mm ? (flat ? 0.0f : span) / (float)p.Kint : 0.0f;
   for (int k = at; k < table_len(p.Kint); k += n) {
@@ -594,8 +615,8 @@ __device__ __forceinline__ void fill_table(const AttnP& p, float2* tab, float sp
     if (flat) {
       if (q >= -1) x.x = up;
     } else if (q >= 0 || (mm && q == -1)) {
-      const float e0 = mm ? expf(fmaf((float)r, h, -span)) : p.e[r];
-      const float e1 = mm ? (r + 1 == p.Kint ? 1.0f : expf(fmaf((float)(r + 1), h, -span))) : p.e[r + 1];
+      const float e0 = mm ? expf(fmaf((float)r, h, -span)) : grid[r];
+      const float e1 = mm ? (r + 1 == p.Kint ? 1.0f : expf(fmaf((float)(r + 1), h, -span))) : grid[r + 1];
       x = q >= 0 ? half_bin(p, q, e0, e1, r, up) : make_float2(up * e0, 0.0f);
     }
     tab[k] = x;
@@ -817,7 +838,7 @@ __device__ __forceinline__ void store_result(const AttnP& p, const RowMap& m, lo
 
 // Rows' maps and tables from final extrema `ext` (R of them, in shared memory); ends with a barrier.
 template <int NT, int MODE>
-__device__ __forceinline__ float prepare_rows(const AttnP& p, const BlockExt<NT>& ext, RowMap* maps, float* tops, float2* tab) {
+__device__ __forceinline__ float prepare_rows(const AttnP& p, const BlockExt<NT>& ext, const float* grid, RowMap* maps, float* tops, float2* tab) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   float up = 1.0f;
   for (int r = warp; r < 8 * NT; r += kWarps) {
@@ -828,9 +849,9 @@ __device__ __forceinline__ float prepare_rows(const AttnP& p, const BlockExt<NT>
       tops[r] = e.x;
     }
     if (MODE == M_GRID && p.calib == CAL_MINMAX)
-      fill_table(p, tab + r * table_len(p.Kint), e.x - e.y, m.flat || m.none, up, lane, 32);
+      fill_table(p, tab + r * table_len(p.Kint), grid, e.x - e.y, m.flat || m.none, up, lane, 32);
   }
-  if (MODE == M_GRID && p.calib != CAL_MINMAX) fill_table(p, tab, 0.0f, false, up, threadIdx.x, kThreads);
+  if (MODE == M_GRID && p.calib != CAL_MINMAX) fill_table(p, tab, grid, 0.0f, false, up, threadIdx.x, kThreads);
   __syncthreads();
   return up;
 }
@@ -926,7 +947,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   float2* tab = reinterpret_cast<float2*>(big + p.big_words);
   __shared__ QTile<D, NT, F32> qt;
   __shared__ float2 wext[kWarps][R];
-  __shared__ float wvs[kWarps], tops[R], bw[R];
+  __shared__ float wvs[kWarps], tops[R], bw[R], grid[KMAX + 1];
   __shared__ BlockExt<NT> mine, ext;
   __shared__ RowMap maps[R];
   __shared__ Sums<D, NT> sums;
@@ -942,18 +963,20 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
     return;
   }
   const int chunk = (u.n + C - 1) / C, i0 = min(rank * chunk, u.n), i1 = min(i0 + chunk, u.n);
+  QRegs<D, NT, F32> q;
+  q.load(p, u);
   const Share sh = share_of(p, u, i0, i1, addr, bad);
   const Ring<D> ring(sm4);
   {
     ring.template prime<true>(sh);
-    if (threadIdx.x == 0) qt.part = reinterpret_cast<__half (*)[R][D + 8]>(big);
-    load_qtile<D, NT, F32>(p, u, qt, reinterpret_cast<__half (*)[R][D + 8]>(big));
+    if (MODE == M_GRID && threadIdx.x <= p.Kint && p.calib != CAL_MINMAX) grid[threadIdx.x] = p.e[threadIdx.x];
+    q.store(p, qt, reinterpret_cast<__half (*)[R][D + 8]>(big));
     __syncthreads();
     Extrema<NT> e;
     key_pass<D, NT, F32, MODE == M_GRID>(p, u, qt, sh, ring, i0, big, e);
+    ring.template prime<false>(sh);
     block_extrema<NT>(e, wext, wvs, mine);
   }
-  ring.template prime<false>(sh);
   if (p.count) {
     float* st = p.stats + (size_t)id * C * (2 * R + 2);
     store_extrema<NT>(st + (size_t)rank * (2 * R + 2), mine);
@@ -982,7 +1005,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
     }
     __syncthreads();
   }
-  const float up = prepare_rows<NT, MODE>(p, C > 1 ? ext : mine, maps, tops, tab);
+  const float up = prepare_rows<NT, MODE>(p, C > 1 ? ext : mine, grid, maps, tops, tab);
   value_pass<D, NT, FOUR, F32, MODE>(p, sh, ring, big, maps, tops, tab, up, big, sums, true);
   if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);
   if (C == 1) {
@@ -1069,12 +1092,12 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attn_scores(const __g
   if (split == 0 && threadIdx.x == 0) p.count[id] = 0;
   const int i0 = split * p.per_split, i1 = min(i0 + p.per_split, u.n);
   if (i0 < i1) {
+    QRegs<D, NT, F32> q;
+    q.load(p, u);
     const Share sh = share_of(p, u, i0, i1, addr, bad);
     const Ring<D> ring(sm4);
     ring.template prime<true>(sh);
-    __half (*part)[R][D + 8] = reinterpret_cast<__half (*)[R][D + 8]>(reinterpret_cast<char*>(sm4) + Ring<D>::kBytes);
-    if (threadIdx.x == 0) qt.part = part;
-    load_qtile<D, NT, F32>(p, u, qt, part);
+    q.store(p, qt, reinterpret_cast<__half (*)[R][D + 8]>(reinterpret_cast<char*>(sm4) + Ring<D>::kBytes));
     __syncthreads();
     Extrema<NT> e;
     key_pass<D, NT, F32, LOW>(p, u, qt, sh, ring, i0, p.scores + ((size_t)id * p.max_slabs + i0) * p.slab_words, e);
@@ -1092,7 +1115,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   float2* tab = reinterpret_cast<float2*>(so + kWarps * R * D);
   __shared__ BlockExt<NT> ext;
   __shared__ RowMap maps[R];
-  __shared__ float tops[R];
+  __shared__ float tops[R], grid[KMAX + 1];
   __shared__ Sums<D, NT> sums;
   __shared__ const uint8_t* addr[kWarps][32];
   __shared__ float wsum[kThreads];
@@ -1112,8 +1135,9 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   const Share sh = share_of(p, u, i0, i1, addr, bad);
   const Ring<D> ring(sm4);
   ring.template prime<false>(sh);
+  if (MODE == M_GRID && threadIdx.x <= p.Kint && p.calib != CAL_MINMAX) grid[threadIdx.x] = p.e[threadIdx.x];
   join_extrema<NT>(p.stats + (size_t)id * p.nsplit * (2 * R + 2), active, ext);
-  const float up = prepare_rows<NT, MODE>(p, ext, maps, tops, tab);
+  const float up = prepare_rows<NT, MODE>(p, ext, grid, maps, tops, tab);
   value_pass<D, NT, FOUR, F32, MODE>(p, sh, ring, p.scores + ((size_t)id * p.max_slabs + i0) * p.slab_words, maps, tops, tab, up, so, sums,
                                false);
   float* part = p.part + ((size_t)id * p.nsplit + split) * (R * (D + 4));
