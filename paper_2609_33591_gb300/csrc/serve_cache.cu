@@ -16,8 +16,8 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Where a channel's partner comes from: nowhere (no rotation), the same eight channels (interleaved), eight channels half the
-// rotation away (one vector), or one by one (half layouts that do not split into eights, and unaligned rows).
+// Where a channel's partner comes from: nowhere (no rotation); the same eight channels (interleaved) or the lane that holds the
+// eight half the rotation away, where a lane's eight are all rotated or none; or one by one from memory (other rotations).
 enum Layout : int { L_NONE = 0, L_INTER = 1, L_HALF = 2, L_ANY = 3 };
 
 // The rotation of a lane's eight channels: y = x c + partner s, the products and the sum rounded one by one (rotate()).
@@ -25,12 +25,14 @@ struct Turn {
   float c[8], s[8];
   int from;       // first channel of the partners (half layout)
   unsigned mask;  // bit i: channel i is rotated
+  bool any;       // some lane's are
 };
 
 __device__ __forceinline__ void load_turn(const CacheIoP& p, int e, int pos, Turn& t) {
   const int half = p.rot >> 1;
   const float2* tab = reinterpret_cast<const float2*>(p.table) + (size_t)pos * half;
   t.mask = 0;
+  t.any = true;
   t.from = e < half ? e + half : e - half;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -62,25 +64,38 @@ __device__ __forceinline__ Chunk<E> fetch(const E* x, bool vec) {
   }
   return a;
 }
-template <class E, int LAYOUT>
+template <class E>
 __device__ __forceinline__ Chunk<E> fetch_partners(const CacheIoP& p, const E* row, int e, const Turn& t) {
-  if constexpr (LAYOUT == L_HALF) return fetch(row + t.from, true);
   const int half = p.rot >> 1;
   Chunk<E> a;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) a.v[i] = (t.mask >> i) & 1u ? row[e + i < half ? e + i + half : e + i - half] : from_f32<E>(0.0f);
+  for (int i = 0; i < 8; ++i) {
+    const int ch = e + i, from = p.interleaved ? ch ^ 1 : (ch < half ? ch + half : ch - half);
+    a.v[i] = (t.mask >> i) & 1u ? row[from] : from_f32<E>(0.0f);
+  }
   return a;
+}
+// The eight channels that lane `from` holds.
+template <class E>
+__device__ __forceinline__ Chunk<E> pass(const Chunk<E>& x, int from) {
+  Chunk<E> y;
+  const uint32_t* a = reinterpret_cast<const uint32_t*>(x.v);
+  uint32_t* b = reinterpret_cast<uint32_t*>(y.v);
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(x.v) / 4; ++i) b[i] = __shfl_sync(0xffffffffu, a[i], from);
+  return y;
 }
 template <class E, int LAYOUT>
 __device__ __forceinline__ void turn(const Turn& t, const Chunk<E>& other, float (&x)[8]) {
-  float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float partner = LAYOUT == L_INTER ? x[i ^ 1] : to_f32(other.v[i]);
-    y[i] = __fadd_rn(__fmul_rn(x[i], t.c[i]), __fmul_rn(partner, t.s[i]));
+  for (int i = 0; i < 8; i += 2) {
+    const float2 a = make_float2(x[i], x[i + 1]);
+    const float2 b = LAYOUT == L_INTER ? make_float2(x[i + 1], x[i]) : make_float2(to_f32(other.v[i]), to_f32(other.v[i + 1]));
+    const float2 u = mul2(a, make_float2(t.c[i], t.c[i + 1])), v = mul2(b, make_float2(t.s[i], t.s[i + 1]));
+    const float2 y = make_float2(__fadd_rn(u.x, v.x), __fadd_rn(u.y, v.y));  // (paired, the sum was fused with the products)
+    x[i] = LAYOUT != L_ANY || ((t.mask >> i) & 1u) ? y.x : x[i];
+    x[i + 1] = LAYOUT != L_ANY || ((t.mask >> i) & 2u) ? y.y : x[i + 1];
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (t.mask >> i) & 1u ? y[i] : x[i];
 }
 
 // Where a slot's rows live: its token's place in its slab, the slab of head 0, and the bytes from one head to the next.
@@ -128,9 +143,11 @@ __device__ __forceinline__ Packed pack8(const float (&x)[8]) {
   // codes in the low bits of the rounded sums: code = bits - bits(kRound), 0 .. 15; added up in base 16 mod 2^32
   uint32_t codes = 0;
 #pragma unroll
-  for (int i = 7; i >= 0; --i) {
-    const float y = fminf(fmaxf(__fmul_rn(__fsub_rn(x[i], c), inv), -8.0f), 7.0f);  // (NaN: -8)
-    codes = codes * 16u + __float_as_uint(__fadd_rn(y, kRound + 8.0f));
+  for (int i = 6; i >= 0; i -= 2) {
+    const float2 y = mul2(add2(make_float2(x[i], x[i + 1]), make_float2(-c, -c)), make_float2(inv, inv));
+    const float2 n = add2(make_float2(fminf(fmaxf(y.x, -8.0f), 7.0f), fminf(fmaxf(y.y, -8.0f), 7.0f)),  // (NaN: -8)
+                          make_float2(kRound + 8.0f, kRound + 8.0f));
+    codes = (codes * 16u + __float_as_uint(n.y)) * 16u + __float_as_uint(n.x);
   }
   return Packed{finite ? codes - 0x4B400000u * 0x11111111u : 0x88888888u, __halves2half2(sh, ch)};
 }
@@ -143,61 +160,70 @@ __device__ __forceinline__ void token_rows(const CacheIoP& p, const Heads& in, i
   int h = first * kRows + lane / kLanes;
   const E* row = reinterpret_cast<const E*>(in.p) + tok * in.st + h * in.sh;
   const long long row_step = step * in.sh;
-  constexpr bool kTurned = KIND != 1 && LAYOUT != L_NONE, kPartners = kTurned && LAYOUT != L_INTER;
-  const bool partners = kPartners && t.mask;
+  constexpr bool kTurned = KIND != 1 && LAYOUT != L_NONE, kPartners = kTurned && LAYOUT == L_ANY;
+  const int from = LAYOUT == L_HALF ? (lane & ~(kLanes - 1)) | (t.from >> 3) : 0;
   uint8_t* slab = at.slab + h * at.head;
   const int g = (e >> 3) & 7;
   uint8_t* code = KIND == 0 ? slab + at.j * (D / 2) + (g & 3) * (D / 8) + 4 * (e >> 5)
                             : slab + 9 * D + 4 * (((at.j >> 1) * 8 + g) * (D / 32) + 2 * (e >> 6)) + 2 * (at.j & 1);
   uint8_t* scale = slab + (KIND ? 17 * D : 8 * D) + (at.j * (D / kGroup) + e / kGroup) * 4;
   E* out = KIND == 2 ? reinterpret_cast<E*>(p.qo.p) + tok * p.qo.st + h * p.qo.sh + e : nullptr;
-  for (int h0 = first * kRows; h0 < in.n; h0 += step, h += step) {
-    Chunk<E> cur, other;
+  constexpr int kBatch = kPartners ? 1 : (sizeof(E) == 2 ? 3 : 2);  // row groups whose loads are under way at once
+  for (int h0 = first * kRows; h0 < in.n; h0 += kBatch * step) {
+    Chunk<E> cur[kBatch], other;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) cur.v[i] = other.v[i] = from_f32<E>(0.0f);
-    if (h < in.n) {
-      cur = fetch(row + e, vec);
-      if (partners) other = fetch_partners<E, LAYOUT>(p, row, e, t);
+    for (int k = 0; k < kBatch; ++k) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) cur[k].v[i] = other.v[i] = from_f32<E>(0.0f);
+      if (h + k * step < in.n) {
+        cur[k] = fetch(row + e, vec);
+        if (kPartners && t.mask) other = fetch_partners(p, row, e, t);
+      }
+      row += row_step;
     }
-    row += row_step;
-    float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = to_f32(cur.v[i]);
-    if (kTurned && t.mask) turn<E, LAYOUT>(t, other, x);
-    if constexpr (KIND == 2) {
-      __syncwarp();  // q_out may be q: every partner has been read
-      if (h < in.n) {
-        if (t.mask == 0) {  // as it is, bit for bit
-          if (vec) {
-            *reinterpret_cast<Chunk<E>*>(out) = cur;
+    for (int k = 0; k < kBatch; ++k, h += step) {
+      if (h0 + k * step >= in.n) break;
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = to_f32(cur[k].v[i]);
+      if (kTurned && LAYOUT == L_HALF && t.any) other = pass(cur[k], from);
+      if (kTurned && t.mask) turn<E, LAYOUT>(t, other, x);
+      if constexpr (KIND == 2) {
+        __syncwarp();  // q_out may be q: every partner has been read
+        if (h < in.n) {
+          if (t.mask == 0) {  // as it is, bit for bit
+            if (vec) {
+              *reinterpret_cast<Chunk<E>*>(out) = cur[k];
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) out[i] = cur[k].v[i];
+            }
           } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) out[i] = cur.v[i];
+            store_ch<E, 8>(out, vec, x);
           }
-        } else {
-          store_ch<E, 8>(out, vec, x);
         }
-      }
-      out += step * p.qo.sh;
-    } else {
-      const Packed k = pack8(x);
-      if (h < in.n) {
-        if constexpr (KIND == 0) {
-          *reinterpret_cast<uint32_t*>(code) = k.codes;
-        } else {
-          reinterpret_cast<uint16_t*>(code)[0] = (uint16_t)k.codes;
-          reinterpret_cast<uint16_t*>(code)[2] = (uint16_t)(k.codes >> 16);
+        out += step * p.qo.sh;
+      } else {
+        const Packed c = pack8(x);
+        if (h < in.n) {
+          if constexpr (KIND == 0) {
+            *reinterpret_cast<uint32_t*>(code) = c.codes;
+          } else {
+            reinterpret_cast<uint16_t*>(code)[0] = (uint16_t)c.codes;
+            reinterpret_cast<uint16_t*>(code)[2] = (uint16_t)(c.codes >> 16);
+          }
+          if ((e & (kGroup - 1)) == 0) *reinterpret_cast<__half2*>(scale) = c.scale;
         }
-        if ((e & (kGroup - 1)) == 0) *reinterpret_cast<__half2*>(scale) = k.scale;
+        code += step * at.head;
+        scale += step * at.head;
       }
-      code += step * at.head;
-      scale += step * at.head;
     }
   }
 }
 
 template <class E, int D, int LAYOUT>
-__global__ void __launch_bounds__(kThreads, sizeof(E) == 2 ? 5 : 3) k_append(const CacheIoP p, bool kvec, bool vvec, bool qvec) {
+__global__ void __launch_bounds__(kThreads, sizeof(E) == 2 ? 4 : 2) k_append(const CacheIoP p, bool kvec, bool vvec, bool qvec) {
   constexpr int kRows = Tile<D>::kRows;
   pdl_trigger();
   pdl_wait();
@@ -215,6 +241,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(E) == 2 ? 5 : 3) k_append(con
   Turn t;
   t.mask = 0;
   t.from = 0;
+  t.any = false;
   if (LAYOUT != L_NONE && turned && ((live && first < kv) || 2 * kv + fq < all)) load_turn(p, e, pos, t);
   if (live) {
     const Place at = place_of(p.c, slot, D);
@@ -305,8 +332,8 @@ cudaError_t append(CacheIoP& p, int nsm, cudaStream_t s) {
   const int grid = warps_for(p, 2 * ((p.c.kv + kRows - 1) / kRows) + (nq + kRows - 1) / kRows, nsm);
   const bool kvec = vec8(p.k, esz), vvec = vec8(p.v, esz), qvec = !p.q.p || (vec8(p.q, esz) && vec8(p.qo, esz));
   if (!p.table) return launch_pdl(k_append<E, D, L_NONE>, dim3(grid), dim3(kThreads), 0, s, p, kvec, vvec, qvec);
-  if (p.interleaved) return launch_pdl(k_append<E, D, L_INTER>, dim3(grid), dim3(kThreads), 0, s, p, kvec, vvec, qvec);
-  if (kvec && qvec && p.rot % 16 == 0) return launch_pdl(k_append<E, D, L_HALF>, dim3(grid), dim3(kThreads), 0, s, p, kvec, vvec, qvec);
+  if (p.interleaved && p.rot % 8 == 0) return launch_pdl(k_append<E, D, L_INTER>, dim3(grid), dim3(kThreads), 0, s, p, kvec, vvec, qvec);
+  if (!p.interleaved && p.rot % 16 == 0) return launch_pdl(k_append<E, D, L_HALF>, dim3(grid), dim3(kThreads), 0, s, p, kvec, vvec, qvec);
   return launch_pdl(k_append<E, D, L_ANY>, dim3(grid), dim3(kThreads), 0, s, p, kvec, vvec, qvec);
 }
 template <class E, int D>
