@@ -35,6 +35,7 @@
 // them in shared memory as 16-bit numbers, four times the bytes that the cache holds.
 #pragma once
 #include <atomic>
+#include <type_traits>
 
 #include "kint_dev.cuh"
 #include "serve_num.cuh"
@@ -274,16 +275,6 @@ __device__ __forceinline__ int score_row(int r, bool four) {  // with the bit th
 }
 __device__ __forceinline__ int score_at(int row, int key) { return (row & ~8) + (key ^ (row & 8)); }
 
-// N consecutive channels of a query row.
-template <int N, bool F32>
-__device__ __forceinline__ void load_q(const AttnP& p, long long off, float (&x)[N]) {
-  if constexpr (F32)
-    load_ch<float, N>(static_cast<const float*>(p.q.p) + off, p.q_vec, x);
-  else if (p.dtype == DT_BF16)
-    load_ch<__nv_bfloat16, N>(static_cast<const __nv_bfloat16*>(p.q.p) + off, p.q_vec, x);
-  else
-    load_ch<__half, N>(static_cast<const __half*>(p.q.p) + off, p.q_vec, x);
-}
 // Four consecutive channels of the output.
 __device__ __forceinline__ void store_o(const AttnP& p, long long off, const float (&x)[4]) {
   if (p.dtype == DT_FP32)
@@ -327,7 +318,8 @@ struct QTile {
 template <int D, int NT, bool F32>
 struct QRegs {
   static constexpr int N = D / 32, kRows = 8 * NT / kWarps;
-  float x[kRows][N];
+  using Raw = typename std::conditional<F32, float, uint16_t>::type;  // 16-bit types are told apart in store()
+  Vec<Raw, N> x[kRows];
   Row row[kRows];
 
   __device__ __forceinline__ void load(const AttnP& p, const Unit& u) {
@@ -337,9 +329,21 @@ struct QRegs {
       const int r = warp + k * kWarps;
       row[k] = row_of(p, u, r);
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[k][i] = 0.0f;
-      if (r < u.rows) load_q<N, F32>(p, row[k].q + lane * N, x[k]);
+      for (int i = 0; i < N; ++i) x[k].v[i] = 0;
+      if (r < u.rows) {
+        const Raw* src = static_cast<const Raw*>(p.q.p) + row[k].q + lane * N;
+        if (p.q_vec) {
+          x[k] = *reinterpret_cast<const Vec<Raw, N>*>(src);
+        } else {
+#pragma unroll
+          for (int i = 0; i < N; ++i) x[k].v[i] = src[i];
+        }
+      }
     }
+  }
+  __device__ __forceinline__ float value(const AttnP& p, int k, int i) const {
+    if constexpr (F32) return x[k].v[i];
+    else return p.dtype == DT_BF16 ? __uint_as_float((uint32_t)x[k].v[i] << 16) : __half2float(__ushort_as_half(x[k].v[i]));
   }
   __device__ __forceinline__ void store(const AttnP& p, QTile<D, NT, F32>& t, __half (*part)[8 * NT][D + 8]) const {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -347,9 +351,12 @@ struct QRegs {
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
       const int r = warp + k * kWarps;
+      float f[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[i] = value(p, k, i);
       float top = 0.0f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(x[k][i]));
+      for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(f[i]));
 #pragma unroll
       for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
       // 2^ex = exponent of top - 13 (top finite and not 0; a subnormal maximum counts as a small normal one)
@@ -359,7 +366,7 @@ struct QRegs {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int ch = lane * N + i;
-        float y = x[k][i] * down;
+        float y = f[i] * down;
         s += y;
         if (!F32 && (ch & 1)) y *= 0.0625f;  // odd nibbles sit at bits 4
         const __half hi = __float2half_rn(y);
