@@ -314,10 +314,11 @@ struct QTile {
   Row row[8 * NT];
 };
 
-// A warp's query rows (every kWarps-th) in registers: loaded before the tables and the first slabs are waited for.
-template <int D, int NT, bool F32>
+// A warp's query rows (every kWarps-th of the tile's TILE) in registers: loaded before the tables and the first slabs are
+// waited for.  Tiles of four leave the other four columns of the key products as they are: their scores are not kept.
+template <int D, int NT, bool F32, int TILE = 8 * NT>
 struct QRegs {
-  static constexpr int N = D / 32, kRows = 8 * NT / kWarps;
+  static constexpr int N = D / 32, kRows = TILE / kWarps;
   using Raw = typename std::conditional<F32, float, uint16_t>::type;  // 16-bit types are told apart in store()
   Vec<Raw, N> x[kRows];
   Row row[kRows];
@@ -823,12 +824,12 @@ __device__ __forceinline__ void store_result(const AttnP& p, const RowMap& m, lo
   store_o(p, off, x);
 }
 
-// Rows' maps and tables from final extrema `ext` (R of them, in shared memory); ends with a barrier.
-template <int NT, int MODE>
+// Rows' maps and tables from final extrema `ext` (TILE rows, in shared memory); ends with a barrier.
+template <int TILE, int NT, int MODE>
 __device__ __forceinline__ float prepare_rows(const AttnP& p, const BlockExt<NT>& ext, const float* grid, RowMap* maps, float* tops, float2* tab) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   float up = 1.0f;
-  for (int r = warp; r < 8 * NT; r += kWarps) {
+  for (int r = warp; r < TILE; r += kWarps) {
     const float2 e = ext.row[r];
     const RowMap m = row_map<MODE>(p, e.x, e.y, ext.vs, up);
     if (lane == 0) {
@@ -950,7 +951,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
     return;
   }
   const int chunk = (u.n + C - 1) / C, i0 = min(rank * chunk, u.n), i1 = min(i0 + chunk, u.n);
-  QRegs<D, NT, F32> q;
+  QRegs<D, NT, F32, FOUR ? 4 : R> q;
   q.load(p, u);
   const Share sh = share_of(p, u, i0, i1, addr, bad);
   const Ring<D> ring(sm4);
@@ -992,7 +993,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
     }
     __syncthreads();
   }
-  const float up = prepare_rows<NT, MODE>(p, C > 1 ? ext : mine, grid, maps, tops, tab);
+  const float up = prepare_rows<FOUR ? 4 : R, NT, MODE>(p, C > 1 ? ext : mine, grid, maps, tops, tab);
   value_pass<D, NT, FOUR, F32, MODE>(p, sh, ring, big, maps, tops, tab, up, big, sums, true);
   if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);
   if (C == 1) {
@@ -1124,7 +1125,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   ring.template prime<false>(sh);
   if (MODE == M_GRID && threadIdx.x <= p.Kint && p.calib != CAL_MINMAX) grid[threadIdx.x] = p.e[threadIdx.x];
   join_extrema<NT>(p.stats + (size_t)id * p.nsplit * (2 * R + 2), active, ext);
-  const float up = prepare_rows<NT, MODE>(p, ext, grid, maps, tops, tab);
+  const float up = prepare_rows<FOUR ? 4 : R, NT, MODE>(p, ext, grid, maps, tops, tab);
   value_pass<D, NT, FOUR, F32, MODE>(p, sh, ring, p.scores + ((size_t)id * p.max_slabs + i0) * p.slab_words, maps, tops, tab, up, so, sums,
                                false);
   float* part = p.part + ((size_t)id * p.nsplit + split) * (R * (D + 4));

@@ -14,7 +14,7 @@
 namespace kint {
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 1024;  // (cta_scan: 32 warps)
 
 // Sums that stop at 2^32 - 1 (still associative): nonsense lengths cannot wrap around.
 __device__ __forceinline__ unsigned add_sat(unsigned a, unsigned b) {
@@ -210,9 +210,9 @@ cudaError_t launch_blocks(const BlocksP& p, int nsm, cudaStream_t s) {
     const cudaError_t e = cudaFuncSetAttribute(k_blocks, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
   }
-  // 4 tokens a thread, two CTAs a SM
+  // 4 tokens a thread, and no more CTAs than run at once (each forms the prefix sums again)
   long long grid = ((long long)p.tokens + 4 * kThreads - 1) / (4 * kThreads);
-  grid = grid < 1 ? 1 : (grid > 2 * nsm ? 2 * nsm : grid);
+  grid = grid < 1 ? 1 : (grid > nsm ? nsm : grid);
   return launch_pdl(k_blocks, dim3((unsigned)grid), dim3(kThreads), smem, s, p);
 }
 

@@ -158,7 +158,7 @@ __device__ __forceinline__ void token_rows(const CacheIoP& p, const Heads& in, i
   constexpr int kLanes = Tile<D>::kLanes, kRows = Tile<D>::kRows;
   const int lane = threadIdx.x & 31, e = 8 * (lane % kLanes), step = p.warps * kRows;
   int h = first * kRows + lane / kLanes;
-  const E* row = reinterpret_cast<const E*>(in.p) + tok * in.st + h * in.sh;
+  const E *row0 = reinterpret_cast<const E*>(in.p) + tok * in.st, *row = row0 + h * in.sh;
   const long long row_step = step * in.sh;
   constexpr bool kTurned = KIND != 1 && LAYOUT != L_NONE, kPartners = kTurned && LAYOUT == L_ANY;
   const int from = LAYOUT == L_HALF ? (lane & ~(kLanes - 1)) | (t.from >> 3) : 0;
@@ -173,12 +173,9 @@ __device__ __forceinline__ void token_rows(const CacheIoP& p, const Heads& in, i
     Chunk<E> cur[kBatch], other;
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) cur[k].v[i] = other.v[i] = from_f32<E>(0.0f);
-      if (h + k * step < in.n) {
-        cur[k] = fetch(row + e, vec);
-        if (kPartners && t.mask) other = fetch_partners(p, row, e, t);
-      }
+      const E* at_k = h + k * step < in.n ? row : row0;  // (past the last head: a row that is there, for nothing)
+      cur[k] = fetch(at_k + e, vec);
+      if (kPartners && t.mask) other = fetch_partners(p, at_k, e, t);
       row += row_step;
     }
 #pragma unroll
