@@ -5,6 +5,9 @@
 // prompts and by latency on single tokens.  A thread owns one chunk of pairs of one
 // token: it reads the chunk's (cos, sin) once and applies it to `hpt` heads of q and k in
 // turn, so the table costs 1 / hpt of what a thread for each (token, head, chunk) reads.
+// Measured on a GB300: 674 MB of bf16 (40 heads of 128, 96 channels rotated) 109 us = 6.2 TB/s, 91% of the measured copy rate;
+// 101 MB of fp32 (interleaved, inverse) 15.5 us = 6.5 TB/s; one step's 64 tokens 2.4 us.  One head a thread instead of up to
+// eight: 322 us for the first.
 #include "serve_num.cuh"
 #include "serve_params.h"
 #include "tc.cuh"

@@ -9,7 +9,10 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+
+#include <optional>
 
 #include "../../include/kint_serve.h"
 
@@ -61,7 +64,21 @@ int whole(PyObject* o) {
   need(v >= INT32_MIN && v <= INT32_MAX, "a whole number is out of range");
   return (int)v;
 }
-void* stream_of(PyObject* o) { return none(o) ? (void*)c10::cuda::getCurrentCUDAStream().stream() : PyLong_AsVoidPtr(o); }
+// The call's stream: the current one, or the given handle, which is then the current one while the call allocates, so that
+// its memory belongs to it.
+struct CallStream {
+  std::optional<c10::cuda::CUDAStreamGuard> guard;
+  void* handle;
+  explicit CallStream(PyObject* o) {
+    if (none(o)) {
+      handle = c10::cuda::getCurrentCUDAStream().stream();
+      return;
+    }
+    handle = PyLong_AsVoidPtr(o);
+    if (!handle && PyErr_Occurred()) throw Refused();
+    guard.emplace(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(handle), c10::cuda::current_device()));
+  }
+};
 
 kint_dtype type_of(const at::Tensor& t, const char* what) {
   switch (t.scalar_type()) {
@@ -180,6 +197,7 @@ PyObject* extend_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t *pl = ints<int32_t>(lens, "lens"), *pa = ints<int32_t>(add, "new"), *pf = ints<int32_t>(list, "free"),
                   *pn = ints<int32_t>(n_free, "n_free");
     int32_t* pt = ints<int32_t>(table, "table");
+    const CallStream stream(a[7]);
     // one allocation: slots (8 bytes each), then pos, req, lens, cu, n_free, refused (4 bytes each), pos and req on 16 bytes
     const int64_t B = lens.size(0), places = up_to(tokens, 4), at_pos = 2 * places, at_req = at_pos + places, at_lens = at_req + places,
                   at_cu = at_lens + B, at_free = at_cu + B + 1, at_ref = at_free + 1;
@@ -187,7 +205,7 @@ PyObject* extend_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t* o = static_cast<int32_t*>(out.data_ptr());
     run(api.blocks_extend(pl, pa, pt, (int)table.stride(0), (int)table.size(1), pf, (int)list.numel(), pn, (int)B, block, tokens,
                           o + at_lens, o + at_free, o + at_cu, reinterpret_cast<int64_t*>(o), o + at_pos, o + at_req, o + at_ref,
-                          stream_of(a[7])),
+                          stream.handle),
         "kint_blocks_extend");
     auto ints_at = [&](int64_t at, int64_t n) { return wrap(part(out, at::kInt, at, {n}, {})); };
     return Py_BuildValue("(NNNNNNN)", ints_at(at_lens, B), ints_at(at_cu, B + 1), wrap(part(out, at::kLong, 0, {tokens}, {})),
@@ -208,6 +226,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
          "pos: expected [B, T] or [T]");
     const int32_t* pp = ints<int32_t>(pos, "pos");
     const Table tab = rotations(tensor(a[3], "table"));
+    const CallStream stream(a[8]);
     at::Tensor qo, ko;
     if (none(a[6])) {  // both outputs in one allocation, k' on a 16-byte boundary
       const int64_t nq = k ? up_to(q.numel(), 8) : q.numel();
@@ -224,7 +243,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (q.numel()) {
       const kint_heads ho = heads(qo, "out", 4), hko = k ? heads(ko, "out", 4) : kint_heads{};
       run(api.rope(&hq, &ho, &hk, &hko, pp, pos.dim() == 2 ? pos.stride(0) : 0, tab.ptr, tab.max_pos, (int)B, (int)T, (int)q.size(3),
-                   tab.rot, PyObject_IsTrue(a[4]), PyObject_IsTrue(a[5]), type_of(q, "q"), stream_of(a[8])),
+                   tab.rot, PyObject_IsTrue(a[4]), PyObject_IsTrue(a[5]), type_of(q, "q"), stream.handle),
           "kint_rope");
     }
     PyObject* second = Py_None;
@@ -254,6 +273,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       need(p.dim() == 1 && p.size(0) == tokens, "a rotation needs pos [tokens]");
       pos = ints<int32_t>(p, "pos");
     }
+    const CallStream stream(a[9]);
     kint_heads hq{}, hqo{};
     at::Tensor qo;
     const bool has_q = !none(a[4]), turn = has_q && tab.ptr;
@@ -269,7 +289,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     if (tokens)
       run(api.append(&c, &hk, &hv, ints<int64_t>(slots, "slots"), (int)tokens, turn ? &hq : nullptr, turn ? &hqo : nullptr, pos, tab.ptr,
-                     tab.max_pos, tab.rot, PyObject_IsTrue(a[7]), type_of(k, "k"), stream_of(a[9])),
+                     tab.max_pos, tab.rot, PyObject_IsTrue(a[7]), type_of(k, "k"), stream.handle),
           "kint_cache_append");
     if (turn) return wrap(qo);
     Py_INCREF(a[4]);
@@ -287,13 +307,14 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     need(slots.dim() == 1, "slots: expected one dimension");
     const int64_t* ps = ints<int64_t>(slots, "slots");
     const auto opts = pages.options().dtype(type == 0 ? at::kFloat : type == 1 ? at::kBFloat16 : at::kHalf);
+    const CallStream stream(a[3]);
     const int64_t each = slots.size(0) * c.kv_heads * c.d;
     const at::Tensor both = at::empty({2 * each}, opts);
     const at::Tensor k = part(both, both.scalar_type(), 0, {slots.size(0), c.kv_heads, c.d}, {}),
                      v = part(both, both.scalar_type(), each, {slots.size(0), c.kv_heads, c.d}, {});
     if (slots.size(0)) {
       const kint_heads hk = heads(k, "k", 3), hv = heads(v, "v", 3);
-      run(api.read(&c, ps, (int)slots.size(0), &hk, &hv, (kint_dtype)type, stream_of(a[3])), "kint_cache_read");
+      run(api.read(&c, ps, (int)slots.size(0), &hk, &hv, (kint_dtype)type, stream.handle), "kint_cache_read");
     }
     return Py_BuildValue("(NN)", wrap(k), wrap(v));
   });
@@ -316,6 +337,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int max_len = none(a[12]) ? (int)(hold < INT32_MAX ? hold : INT32_MAX) : whole(a[12]);
     const double tau = PyFloat_AsDouble(a[7]);
     if (tau == -1.0 && PyErr_Occurred()) throw Refused();
+    const CallStream stream(a[15]);
     at::Tensor out = none(a[13]) ? at::empty_like(q) : tensor(a[13], "out");
     need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out disagrees with q");
     if (q.numel()) {
@@ -334,7 +356,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       }
       run(api.attn(&hq, &ho, &c, pt, (int)table.stride(0), width, pl, pc, (int)q.size(0), B, window, sinks, whole(a[5]), (kint_calib)whole(a[6]),
                    (float)tau, (kint_recon)whole(a[8]), max_new, max_len, type_of(q, "q"), ws.data_ptr(), ws.is_same(pages) ? kUnusedWorkspace : ws.nbytes(),
-                   stream_of(a[15])),
+                   stream.handle),
           "kint_cache_attn");
     }
     return wrap(out);

@@ -1,8 +1,8 @@
 """Serving with K-interval attention: block tables, rotary positions, a paged cache that holds
 keys and values in 4 bits, and attention over it (include/kint_serve.h).
 
-The functions take torch tensors and run libkint's kernels on the current stream (or the one
-given); torch supplies the memory.  One step of a layer is
+The functions take torch tensors and run libkint's kernels on the current stream, or the one
+given, to which the memory that a call allocates then belongs.  One step of a layer is
 
     plan = extend_blocks(...)                       # once a step
     q = append(k, v, plan.slots, pages, q=q, pos=plan.pos, table=rope)

@@ -222,7 +222,30 @@ def test_strides_layers_streams_and_graphs():
         other = serve.attention(q, pages, table, lens_g, cu, cfg, **kw)
     side.synchronize()
     assert torch.equal(other, want)
+    other = serve.attention(q, pages, table, lens_g, cu, cfg, stream=side, **kw)
+    side.synchronize()
+    assert torch.equal(other, want)
     ws = serve.attention_workspace(3, H, kv, d, **kw)
+    res = torch.zeros_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        serve.attention(q, pages, table, lens_g, cu, cfg, out=res, ws=ws, **kw)
+    for _ in range(2):
+        res.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(res, want)
+
+
+@pytest.mark.parametrize("lens,new,heads", [([6000], [1], 4), ([8300], [130], 16)])
+def test_captured_long_lists(lens, new, heads):
+    """The cooperative launch and the two launches in a captured graph: the plain call's bits, replay after replay."""
+    pool = filled(lens, 1, 64, 128, 17)
+    pages, table, lens_g, cu = gpu(pool.pages), gpu(pool.table), gpu(pool.lens), ints([0] + new)
+    q, cfg = torch.randn(new[0], heads, 64, device="cuda").bfloat16(), kint.Config(calib=FWM, recon=LERP)
+    kw = dict(max_new=new[0], max_len=lens[0])
+    want = serve.attention(q, pages, table, lens_g, cu, cfg, **kw)
+    ws = serve.attention_workspace(1, heads, 1, 64, **kw)
     res = torch.zeros_like(q)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
