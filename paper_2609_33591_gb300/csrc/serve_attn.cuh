@@ -884,48 +884,65 @@ __device__ __forceinline__ float4 peer_f32x4(uint32_t a) {
 // All `blocks` blocks of a unit have come here (a cooperative launch: they run at once); what they wrote before is visible.
 // The wait is bounded: past the limit it flags the status word and goes on.
 __device__ __forceinline__ void unit_sync(const AttnP& p, int* counter, int blocks) {
-  __threadfence();
-  __syncthreads();
+  __syncthreads();  // the block's writes come before thread 0's fence, which orders them before its arrival
   if (threadIdx.x == 0) {
+    __threadfence();
     atomicAdd(counter, 1);
     const uint64_t t0 = globaltimer_ns();
     int seen;
-    while (true) {
+    for (int poll = 1;; ++poll) {
       asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
       if (seen >= blocks) break;
-      if (globaltimer_ns() - t0 > p.wait_ns) {
+      if (poll % 64 == 0 && globaltimer_ns() - t0 > p.wait_ns) {
         dev_flag(p.status, DEV_ERR_TIMEOUT_SYNC);
         break;
       }
-      __nanosleep(40);
+      __nanosleep(20);
     }
+    __threadfence();
   }
   __syncthreads();
-  __threadfence();
 }
-// The extrema of a unit's `n` ranges, st[range][2 R + 2] (ends with a barrier).
-template <int NT>
+// The extrema of a unit's `n` ranges for the first TILE rows, st[range][2 R + 2] (ends with a barrier).  A warp's loads are
+// issued together, four ranges a lane and all of its rows at a time.
+template <int TILE, int NT>
 __device__ __forceinline__ void join_extrema(const float* st, int n, BlockExt<NT>& ext) {
-  constexpr int R = 8 * NT;
+  constexpr int R = 8 * NT, kMine = (TILE + kWarps) / kWarps;  // rows a warp, the V scales (row R) among them
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int r = warp; r <= R; r += kWarps) {  // row R: the V scales
-    float a = r < R ? kMasked : 0.0f, b = INFINITY;
-    for (int s = lane; s < n; s += 32) {
-      const float2 x = __ldcg(reinterpret_cast<const float2*>(st + (size_t)s * (2 * R + 2) + 2 * r));
-      a = max_nan(a, x.x);
-      b = fminf(b, x.y);
+  float a[kMine], b[kMine];
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    a[k] = kMasked;
+    b[k] = INFINITY;
+  }
+  for (int s0 = lane; s0 < n; s0 += 128) {
+    float2 x[kMine][4];
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      const int r = warp + k * kWarps, at = r < TILE ? 2 * r : 2 * R;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x[k][j] = s0 + 32 * j < n ? __ldcg(reinterpret_cast<const float2*>(st + (size_t)(s0 + 32 * j) * (2 * R + 2) + at))
+                                  : make_float2(kMasked, INFINITY);
     }
 #pragma unroll
+    for (int k = 0; k < kMine; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        a[k] = max_nan(a[k], x[k][j].x);
+        b[k] = fminf(b[k], x[k][j].y);
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int r = warp + k * kWarps;
+#pragma unroll
     for (int o = 16; o; o >>= 1) {
-      a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
-      b = fminf(b, __shfl_xor_sync(0xffffffffu, b, o));
+      a[k] = max_nan(a[k], __shfl_xor_sync(0xffffffffu, a[k], o));
+      b[k] = fminf(b[k], __shfl_xor_sync(0xffffffffu, b[k], o));
     }
-    if (lane == 0) {
-      if (r < R)
-        ext.row[r] = make_float2(a, b);
-      else
-        ext.vs = a;
-    }
+    if (lane == 0 && r < TILE) ext.row[r] = make_float2(a[k], b[k]);
+    if (lane == 0 && r == TILE) ext.vs = a[k];
   }
   __syncthreads();
 }
@@ -978,7 +995,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
     float* st = p.stats + (size_t)id * C * (2 * R + 2);
     store_extrema<NT>(st + (size_t)rank * (2 * R + 2), mine);
     unit_sync(p, p.count + 2 * id, C);
-    join_extrema<NT>(st, C, ext);
+    join_extrema<FOUR ? 4 : R, NT>(st, C, ext);
   } else if (C > 1) {
     cluster_arrive();
     cluster_wait();
@@ -1026,11 +1043,20 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
       const int r = x / V, d = 4 * (x % V);
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
       float W = 0.0f;
-      for (int c = lane; c < C; c += 32) {
-        const float* a = all + (size_t)c * (R * (D + 4)) + r * (D + 4);
-        const float4 y = __ldcg(reinterpret_cast<const float4*>(a + d));
-        o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
-        W += __ldcg(a + D);
+      for (int c0 = lane; c0 < C; c0 += 128) {
+        float4 y[4];
+        float w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float* a = all + (size_t)(c0 + 32 * j) * (R * (D + 4)) + r * (D + 4);
+          y[j] = c0 + 32 * j < C ? __ldcg(reinterpret_cast<const float4*>(a + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          w[j] = c0 + 32 * j < C ? __ldcg(a + D) : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          o.x += y[j].x; o.y += y[j].y; o.z += y[j].z; o.w += y[j].w;
+          W += w[j];
+        }
       }
 #pragma unroll
       for (int k = 16; k; k >>= 1) {
@@ -1133,7 +1159,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   const Ring<D> ring(sm4);
   ring.template prime<false>(sh);
   if (MODE == M_GRID && threadIdx.x <= p.Kint && p.calib != CAL_MINMAX) grid[threadIdx.x] = p.e[threadIdx.x];
-  join_extrema<NT>(p.stats + (size_t)id * p.nsplit * (2 * R + 2), active, ext);
+  join_extrema<FOUR ? 4 : R, NT>(p.stats + (size_t)id * p.nsplit * (2 * R + 2), active, ext);
   const float up = prepare_rows<FOUR ? 4 : R, NT, MODE>(p, ext, grid, maps, tops, tab);
   value_pass<D, NT, FOUR, F32, MODE>(p, sh, ring, p.scores + ((size_t)id * p.max_slabs + i0) * p.slab_words, maps, tops, tab, up, so, sums,
                                false);
