@@ -305,7 +305,7 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
   p.o_vec = reinterpret_cast<uintptr_t>(out->ptr) % vec == 0 && out->stride_t % 4 == 0 && out->stride_h % 4 == 0;
   char* ws = static_cast<char*>(workspace);
   p.scores = reinterpret_cast<float*>(ws + a.scores);
-  p.stats = reinterpret_cast<float*>(ws + a.stats);
+  p.stats = reinterpret_cast<float2*>(ws + a.stats);
   p.part = reinterpret_cast<float*>(ws + a.part);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   auto launch = [&](int what) { return cache->d == 128 ? launch_attn_128(p, what, s) : launch_attn_64(p, what, s); };

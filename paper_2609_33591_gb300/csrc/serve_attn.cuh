@@ -903,10 +903,11 @@ __device__ __forceinline__ void unit_sync(const AttnP& p, int* counter, int bloc
   }
   __syncthreads();
 }
-// The extrema of a unit's `n` ranges for the first TILE rows, st[range][2 R + 2] (ends with a barrier).  A warp's loads are
-// issued together, four ranges a lane and all of its rows at a time.
+// The extrema of the first `n` of a unit's `all` ranges for the first TILE rows (ends with a barrier).  st is [R + 1][all]: a
+// row's ranges lie side by side, so that a load instruction of a warp touches 256 bytes in a row and not 32 lines, and a
+// warp's loads are issued together, four ranges a lane and all of its rows at a time.
 template <int TILE, int NT>
-__device__ __forceinline__ void join_extrema(const float* st, int n, BlockExt<NT>& ext) {
+__device__ __forceinline__ void join_extrema(const float2* st, int all, int n, BlockExt<NT>& ext) {
   constexpr int R = 8 * NT, kMine = (TILE + kWarps) / kWarps;  // rows a warp, the V scales (row R) among them
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   float a[kMine], b[kMine];
@@ -919,11 +920,10 @@ __device__ __forceinline__ void join_extrema(const float* st, int n, BlockExt<NT
     float2 x[kMine][4];
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
-      const int r = warp + k * kWarps, at = r < TILE ? 2 * r : 2 * R;
+      const float2* row = st + (size_t)(warp + k * kWarps < TILE ? warp + k * kWarps : R) * all;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        x[k][j] = s0 + 32 * j < n ? __ldcg(reinterpret_cast<const float2*>(st + (size_t)(s0 + 32 * j) * (2 * R + 2) + at))
-                                  : make_float2(kMasked, INFINITY);
+        x[k][j] = s0 + 32 * j < n ? __ldcg(row + s0 + 32 * j) : make_float2(kMasked, INFINITY);
     }
 #pragma unroll
     for (int k = 0; k < kMine; ++k)
@@ -947,10 +947,10 @@ __device__ __forceinline__ void join_extrema(const float* st, int n, BlockExt<NT
   __syncthreads();
 }
 template <int NT>
-__device__ __forceinline__ void store_extrema(float* st, const BlockExt<NT>& mine) {
+__device__ __forceinline__ void store_extrema(float2* st, int all, int range, const BlockExt<NT>& mine) {
   constexpr int R = 8 * NT;
-  if (threadIdx.x < R) *reinterpret_cast<float2*>(st + 2 * threadIdx.x) = mine.row[threadIdx.x];
-  if (threadIdx.x == 32) *reinterpret_cast<float2*>(st + 2 * R) = make_float2(mine.vs, 0.0f);
+  if (threadIdx.x < R) st[(size_t)threadIdx.x * all + range] = mine.row[threadIdx.x];
+  if (threadIdx.x == 32) st[(size_t)R * all + range] = make_float2(mine.vs, 0.0f);
 }
 
 template <int D, int NT, bool FOUR, bool F32, int MODE>
@@ -992,10 +992,10 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
     block_extrema<NT>(e, wext, wvs, mine);
   }
   if (p.count) {
-    float* st = p.stats + (size_t)id * C * (2 * R + 2);
-    store_extrema<NT>(st + (size_t)rank * (2 * R + 2), mine);
+    float2* st = p.stats + (size_t)id * C * (R + 1);
+    store_extrema<NT>(st, C, rank, mine);
     unit_sync(p, p.count + 2 * id, C);
-    join_extrema<FOUR ? 4 : R, NT>(st, C, ext);
+    join_extrema<FOUR ? 4 : R, NT>(st, C, C, ext);
   } else if (C > 1) {
     cluster_arrive();
     cluster_wait();
@@ -1029,44 +1029,49 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
     }
     return;
   }
-  if (p.count) {  // this block's sums into the workspace; then the unit's warps join four channels each, a lane every 32nd block
+  // Sums through the workspace, [block][R][D], and the rows' weights behind them, [R][block].  A warp joins eight channels:
+  // two lanes a block, so that both halves of a 32-byte sector go to one load, and 16 blocks a load instruction.
+  if (p.count) {
     float* all = p.part + (size_t)id * C * (R * (D + 4));
-    float* part = all + (size_t)rank * (R * (D + 4));
+    float* weights = all + (size_t)C * R * D;
     for (int x = threadIdx.x; x < u.rows * V; x += kThreads) {
       const int r = x / V, d = 4 * (x % V);
-      *reinterpret_cast<float4*>(part + r * (D + 4) + d) = block_sum<D, NT, FOUR>(big, sums, r, d);
-      if (d == 0) part[r * (D + 4) + D] = block_weight<D, NT>(sums, r);
+      *reinterpret_cast<float4*>(all + (size_t)(rank * R + r) * D + d) = block_sum<D, NT, FOUR>(big, sums, r, d);
+      if (d == 0) weights[r * C + rank] = block_weight<D, NT>(sums, r);
     }
     unit_sync(p, p.count + 2 * id + 1, C);
     const int lane = threadIdx.x & 31;
-    for (int x = rank * kWarps + warp_id_uniform(); x < u.rows * V; x += C * kWarps) {
-      const int r = x / V, d = 4 * (x % V);
+    for (int x = rank + C * warp_id_uniform(); x < u.rows * (V / 2); x += C * kWarps) {
+      const int r = x / (V / 2), d = 8 * (x % (V / 2)) + 4 * (lane & 1);
+      const float* a = all + (size_t)r * D + d;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
       float W = 0.0f;
-      for (int c0 = lane; c0 < C; c0 += 128) {
-        float4 y[4];
+      for (int c0 = 0; c0 < C; c0 += 128) {
+        float4 y[8];
         float w[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float* a = all + (size_t)(c0 + 32 * j) * (R * (D + 4)) + r * (D + 4);
-          y[j] = c0 + 32 * j < C ? __ldcg(reinterpret_cast<const float4*>(a + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
-          w[j] = c0 + 32 * j < C ? __ldcg(a + D) : 0.0f;
+        for (int j = 0; j < 8; ++j) {
+          const int c = c0 + 16 * j + (lane >> 1);
+          y[j] = c < C ? __ldcg(reinterpret_cast<const float4*>(a + (size_t)c * (R * D))) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 4; ++j) w[j] = c0 + 32 * j + lane < C ? __ldcg(weights + r * C + c0 + 32 * j + lane) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
           o.x += y[j].x; o.y += y[j].y; o.z += y[j].z; o.w += y[j].w;
-          W += w[j];
         }
+        W += (w[0] + w[1]) + (w[2] + w[3]);
       }
 #pragma unroll
-      for (int k = 16; k; k >>= 1) {
+      for (int k = 16; k > 1; k >>= 1) {
         o.x += __shfl_xor_sync(0xffffffffu, o.x, k);
         o.y += __shfl_xor_sync(0xffffffffu, o.y, k);
         o.z += __shfl_xor_sync(0xffffffffu, o.z, k);
         o.w += __shfl_xor_sync(0xffffffffu, o.w, k);
-        W += __shfl_xor_sync(0xffffffffu, W, k);
       }
-      if (lane == 0) store_result(p, maps[r], qt.row[r].o + d, o, W);
+#pragma unroll
+      for (int k = 16; k; k >>= 1) W += __shfl_xor_sync(0xffffffffu, W, k);
+      if (lane < 2) store_result(p, maps[r], qt.row[r].o + d, o, W);
     }
     return;
   }
@@ -1125,7 +1130,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attn_scores(const __g
     Extrema<NT> e;
     key_pass<D, NT, F32, LOW>(p, u, qt, sh, ring, i0, p.scores + ((size_t)id * p.max_slabs + i0) * p.slab_words, e);
     block_extrema<NT>(e, wext, wvs, mine);
-    store_extrema<NT>(p.stats + ((size_t)id * p.nsplit + split) * (2 * R + 2), mine);
+    store_extrema<NT>(p.stats + (size_t)id * p.nsplit * (R + 1), p.nsplit, split, mine);
   }
   if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);
 }
@@ -1159,7 +1164,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   const Ring<D> ring(sm4);
   ring.template prime<false>(sh);
   if (MODE == M_GRID && threadIdx.x <= p.Kint && p.calib != CAL_MINMAX) grid[threadIdx.x] = p.e[threadIdx.x];
-  join_extrema<FOUR ? 4 : R, NT>(p.stats + (size_t)id * p.nsplit * (2 * R + 2), active, ext);
+  join_extrema<FOUR ? 4 : R, NT>(p.stats + (size_t)id * p.nsplit * (R + 1), p.nsplit, active, ext);
   const float up = prepare_rows<FOUR ? 4 : R, NT, MODE>(p, ext, grid, maps, tops, tab);
   value_pass<D, NT, FOUR, F32, MODE>(p, sh, ring, p.scores + ((size_t)id * p.max_slabs + i0) * p.slab_words, maps, tops, tab, up, so, sums,
                                false);

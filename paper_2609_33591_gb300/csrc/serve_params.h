@@ -92,8 +92,8 @@ struct AttnP {
   int slab_words;                    // scores kept a slab: 128 nt, or 64 for tiles of at most four rows
   int big_words;                     // one launch: floats of a block's scores, or of its partial sums where those are more
   float* scores;                     // [unit][max_slabs][slab_words]
-  float* stats;                      // [unit][nsplit][nt * 16 + 2]: extrema of each row, the largest V scale
-  float* part;                       // [unit][nsplit][nt * 8][d + 1]
+  float2* stats;                     // [unit][nt * 8 + 1][nsplit]: extrema of each row, the largest V scale
+  float* part;                       // [unit]: two launches [nsplit][nt * 8][d + 4], the weight behind a row; else sums, then weights
   int* count;                        // one cooperative launch: [unit][2], zero before it; two launches: [unit]
   unsigned long long wait_ns;        // limit of a wait for the other blocks
   FastDiv by_tiles, by_kv, by_G;
