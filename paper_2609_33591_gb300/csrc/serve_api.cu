@@ -73,7 +73,8 @@ constexpr int kSms = 152;
 constexpr int kBlocksPerSm = 16 / kAttnWarps;          // of at most 128 registers a thread
 constexpr int kScoreWords = 8192;                      // 32 KB of scores a block, beside 20 KB of copies in flight
 constexpr int kBlockSlabs = 32 * kAttnWarps;           // a warp keeps the addresses of 32
-constexpr int kMinSlabs = 8 * kAttnWarps;              // fewest slabs a block that splitting leaves
+constexpr int kMinSlabs = 2 * kAttnWarps;              // fewest slabs a block that splitting a unit over a cluster leaves
+constexpr int kMinCoop = 8 * kAttnWarps;               // and over a cooperative launch
 
 bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int sinks, int max_new, int max_len) {
   if (B < 1 || q_heads < 1 || kv < 1 || q_heads % kv || (d != 64 && d != 128) || window < 0 || sinks < 0 || max_new < 1 ||
@@ -94,14 +95,18 @@ bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int s
   const long long most = std::min(kScoreWords / a.slab_words, kBlockSlabs);
   const int sums = kAttnWarps * 8 * a.nt * d;
   // A cluster of up to 8 blocks a unit, 32 KB of scores a block (kBlocksPerSm blocks a SM) or, past what 8 such blocks hold,
-  // 64 KB.  A block costs about 5 us of latency whatever it does, so a unit is split further only while all blocks still
-  // run at once and each has kMinSlabs.
+  // 64 KB.  A block costs about 5 us of latency whatever it does, so a unit is split further only while all blocks still run
+  // at once and each has kMinSlabs; any number of blocks, not only powers of two (d = 128, 4 rows: 96 units of 8192 keys, 6
+  // blocks a unit for 4: 43.8 -> 33.7 us; 192 of 2000, 3 for 2: 25.4 -> 20.4).  80 units of 600 keys with 8, 16 and 24
+  // slabs at least: 11.5, 13.1 and 12.5 us; one slab a warp gains nothing more.
   const long long slots = (long long)kSms * (a.nt == 2 && d == 128 ? 3 * kBlocksPerSm / 4 : kBlocksPerSm);
   int c = (int)std::min<long long>((slabs + most - 1) / most, 8);
   a.shape = slabs <= c * std::min<long long>(2 * most, kBlockSlabs) ? SHAPE_CLUSTER : SHAPE_TWO;
-  while (a.shape == SHAPE_CLUSTER && 2 * c <= 8 && units * c * 2 <= slots && slabs >= kMinSlabs * c) c *= 2;
-  // Where the units are so few that twice those blocks and more run at once, a cooperative launch.
-  const long long coop = units > slots ? 0 : std::min(slots / units, (slabs + kMinSlabs - 1) / kMinSlabs);
+  if (a.shape == SHAPE_CLUSTER) c = (int)std::max<long long>(c, std::min({8ll, slots / units, slabs / kMinSlabs}));
+  // Where the units are so few that twice those blocks and more run at once, a cooperative launch.  (Its exchange is dearer:
+  // 64 units of 8192 keys take 31.0 us with 9 blocks a unit so, 26.6 as clusters of 8; 16 slabs a block at least: 32 units
+  // of 4096 keys 19.7 us, 32: 17.0.)
+  const long long coop = units > slots ? 0 : std::min(slots / units, (slabs + kMinCoop - 1) / kMinCoop);
   if (coop >= 2 * c && slabs <= coop * most) {
     a.shape = SHAPE_COOP;
     c = (int)coop;
@@ -114,9 +119,9 @@ bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int s
     a.bytes = 256;  // (not touched)
     return units * c <= 0x7fffffffll;
   }
-  // Two launches: 64 slabs a block, fewer while the grid is under two blocks a SM, 8 at least.  (A cooperative launch that the
-  // device has no room for runs so too.)
-  long long per = 64;
+  // Two launches: 128 slabs a block (64: 240 units of 30000 keys 337 us, 128: 313), fewer while the grid is under two blocks a
+  // SM, 8 at least.  (A cooperative launch that the device has no room for runs so too.)
+  long long per = 128;
   while (per > 8 && units * ((slabs + per - 1) / per) < 2 * kSms) per >>= 1;
   const long long nsplit = (slabs + per - 1) / per;
   if (units * nsplit > 0x7fffffffll) return false;
