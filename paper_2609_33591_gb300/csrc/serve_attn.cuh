@@ -327,9 +327,10 @@ struct QTile {
 // waited for.  Tiles of four leave the other four columns of the key products as they are: their scores are not kept.
 template <int D, int NT, bool F32, int TILE = 8 * NT>
 struct QRegs {
-  static constexpr int N = D / 32, kRows = TILE / kWarps;
-  using Raw = typename std::conditional<F32, float, uint16_t>::type;  // 16-bit types are told apart in store()
-  Vec<Raw, N> x[kRows];
+  static constexpr int N = D / 32, kRows = TILE / kWarps, kWords = F32 ? N : N / 2;
+  using Raw = typename std::conditional<F32, uint32_t, uint16_t>::type;
+  // As words, told apart into elements in store(): taking them apart here would wait for each row before the next is asked for.
+  Vec<uint32_t, kWords> x[kRows];
   Row row[kRows];
 
   __device__ __forceinline__ void load(const AttnP& p, const Unit& u) {
@@ -339,21 +340,23 @@ struct QRegs {
       const int r = warp + k * kWarps;
       row[k] = row_of(p, u, r);
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[k].v[i] = 0;
+      for (int i = 0; i < kWords; ++i) x[k].v[i] = 0;
       if (r < u.rows) {
         const Raw* src = static_cast<const Raw*>(p.q.p) + row[k].q + lane * N;
         if (p.q_vec) {
-          x[k] = *reinterpret_cast<const Vec<Raw, N>*>(src);
+          x[k] = *reinterpret_cast<const Vec<uint32_t, kWords>*>(src);
         } else {
 #pragma unroll
-          for (int i = 0; i < N; ++i) x[k].v[i] = src[i];
+          for (int i = 0; i < kWords; ++i) x[k].v[i] = F32 ? src[i] : (uint32_t)src[2 * i] | (uint32_t)src[2 * i + 1] << 16;
         }
       }
     }
   }
   __device__ __forceinline__ float value(const AttnP& p, int k, int i) const {
-    if constexpr (F32) return x[k].v[i];
-    else return p.dtype == DT_BF16 ? __uint_as_float((uint32_t)x[k].v[i] << 16) : __half2float(__ushort_as_half(x[k].v[i]));
+    if constexpr (F32) return __uint_as_float(x[k].v[i]);
+    const uint32_t w = x[k].v[i / 2];
+    if (p.dtype == DT_BF16) return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+    return __half2float(__ushort_as_half((unsigned short)(i & 1 ? w >> 16 : w)));
   }
   __device__ __forceinline__ void store(const AttnP& p, QTile<D, NT, F32>& t, __half (*part)[8 * NT][D + 8]) const {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
