@@ -140,6 +140,14 @@ def test_few_units_with_long_lists(heads, new, d):
     check_attention([4100, 0, 3], [new, 0, min(new, 3)], heads, 1, d, cfg, F32, block=64, seed=15)
 
 
+@pytest.mark.parametrize("blocks", range(1, 9))
+@pytest.mark.parametrize("heads,d,dtype", [(4, 64, F32), (7, 128, BF16), (13, 64, BF16)])
+def test_every_number_of_blocks_a_unit(blocks, heads, d, dtype):
+    """Eight slabs a thread block: clusters of one to eight; a request too short for all of them and an empty one beside it."""
+    cfg = kint.Config(Kint=8, calib=MM, recon=LERP)
+    check_attention([128 * blocks + 5, 19, 0], [1, 1, 0], heads, 1, d, cfg, dtype, seed=17 + blocks)
+
+
 def test_many_tiles_with_long_lists():
     """Scores too many for shared memory: two launches, joined by the last block of each tile."""
     check_attention([8500], [150], 16, 1, 64, kint.Config(calib=SOFT), F32, block=256, seed=16)
