@@ -8,8 +8,8 @@
 // warp works on 256 channels: two heads of 128, four of 64.  A warp stays with one token:
 // its slot, position and rotation are loaded once for all the heads it takes.  Several warps a token were slower on prompts
 // (one 137 us, six 205 us, in an earlier form of the loop below).
-// Measured on a GB300, 16381 tokens of 24 + 24 + 24 heads of 64 in bf16: append 63 us (interleaved rotation; 71 us half) for 229 MB
-// = 3.6 TB/s, bound by instruction issue (71% of the slots; 178 instructions for 256 channels), read back 27 us for 129 MB =
+// Measured on a GB300, 16381 tokens of 24 + 24 + 24 heads of 64 in bf16: append 62 us (interleaved rotation; 69 us half) for 229 MB
+// = 3.7 TB/s, bound by instruction issue (69% of the slots; some 170 instructions for 256 channels), read back 27 us for 129 MB =
 // 4.8 TB/s; one step's 64 tokens 3.8 and 2.4 us.
 #include "serve_num.cuh"
 
@@ -122,23 +122,55 @@ struct Tile {
   static constexpr int kLanes = D / 8, kRows = 32 / kLanes;
 };
 
+// The least of three; the largest, NaN where one is.
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float d;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // Codes of a group's eight channels x, from its s and c.
 struct Packed {
   uint32_t codes;
   __half2 scale;
 };
-__device__ __forceinline__ Packed pack8(const float (&x)[8]) {
-  float lo = x[0], hi = x[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) {
-    lo = fminf(lo, x[i]);
-    hi = max_nan(hi, x[i]);
-  }
+// The extrema of a group (NaN: hi is NaN) from a lane's eight channels.
+__device__ __forceinline__ void extrema(const float (&x)[8], float& lo, float& hi) {
+  lo = fminf(min3(min3(x[0], x[1], x[2]), x[3], x[4]), min3(x[5], x[6], x[7]));
+  hi = max_nan(max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[4]), max3_nan(x[5], x[6], x[7]));
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) {
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
   }
+}
+// The same from 16-bit channels as they came, two to a word: after the lane's own, one word carries (lo, -hi), so the group
+// takes half the shuffles (values without a rotation: 38.8 -> 38.0 us, with one of the keys, half layout, 71.6 -> 68.6).
+__device__ __forceinline__ __half2 pair(uint32_t w, __half) { return *reinterpret_cast<const __half2*>(&w); }
+__device__ __forceinline__ __nv_bfloat162 pair(uint32_t w, __nv_bfloat16) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+template <class E>
+__device__ __forceinline__ void extrema(const Chunk<E>& x, float& lo, float& hi) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(x.v);
+  auto least = [](uint32_t a, uint32_t b) {
+    const auto m = __hmin2_nan(pair(a, E()), pair(b, E()));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  };
+  const uint32_t a = least(least(w[0], w[1]), least(w[2], w[3]));
+  constexpr uint32_t kSigns = 0x80008000u;
+  const uint32_t b = least(least(w[0] ^ kSigns, w[1] ^ kSigns), least(w[2] ^ kSigns, w[3] ^ kSigns));
+  uint32_t m = least(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) m = least(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const auto both = pair(m, E());
+  lo = to_f32(both.x);
+  hi = -to_f32(both.y);
+}
+__device__ __forceinline__ Packed pack8(const float (&x)[8], float lo, float hi) {
   const bool finite = hi < INFINITY && lo > -INFINITY;  // (a NaN makes hi NaN)
   const __half sh = finite ? half_sat(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)) : __ushort_as_half(0);
   const float s = __half2float(sh);
@@ -206,7 +238,10 @@ __device__ __forceinline__ void token_rows(const CacheIoP& p, const Heads& in, i
         }
         out += step * p.qo.sh;
       } else {
-        const Packed c = pack8(x);
+        float lo, hi;
+        if constexpr (sizeof(E) == 2 && !kTurned) extrema<E>(cur[k], lo, hi);
+        else extrema(x, lo, hi);
+        const Packed c = pack8(x, lo, hi);
         if (h < in.n) {
           if constexpr (KIND == 0) {
             *reinterpret_cast<uint32_t*>(code) = c.codes;
