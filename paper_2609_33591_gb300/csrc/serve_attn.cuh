@@ -491,10 +491,11 @@ __device__ __forceinline__ void key_pass(const AttnP& p, const Unit& u, const QT
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const float v = s[n][c] * mul[n][c & 1];
-          e.hi[n][c & 1] = max_nan(e.hi[n][c & 1], v);
-          if constexpr (LOW) e.lo[n][c & 1] = fminf(e.lo[n][c & 1], v);
-          if (keep) o[n * 128 + score_at(c & 1 ? out1 : out0, g + (c >= 2 ? 8 : 0))] = v;
+          s[n][c] *= mul[n][c & 1];
+          if (keep) o[n * 128 + score_at(c & 1 ? out1 : out0, g + (c >= 2 ? 8 : 0))] = s[n][c];
+          if (c < 2) continue;
+          e.hi[n][c & 1] = max3_nan(e.hi[n][c & 1], s[n][c - 2], s[n][c]);
+          if constexpr (LOW) e.lo[n][c & 1] = min3(e.lo[n][c & 1], s[n][c - 2], s[n][c]);
         }
     } else {  // a slab at the end of what is seen, or with a bad block number
       const bool ok = (sh.oks >> l) & 1u;

@@ -122,18 +122,6 @@ struct Tile {
   static constexpr int kLanes = D / 8, kRows = 32 / kLanes;
 };
 
-// The least of three; the largest, NaN where one is.
-__device__ __forceinline__ float min3(float a, float b, float c) {
-  float d;
-  asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {
-  float d;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-
 // Codes of a group's eight channels x, from its s and c.
 struct Packed {
   uint32_t codes;

@@ -73,6 +73,18 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
+// The least of three; the largest, NaN where one is.
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float d;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // Pairs of fp32 in one instruction.
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   float2 r;
