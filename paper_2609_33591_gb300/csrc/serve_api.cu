@@ -66,6 +66,7 @@ struct AttnPlan {
   int G, nt, tiles, max_slabs, slab_words, shape;
   int blocks, big_words;  // one launch: blocks a unit, floats of shared memory a block keeps scores (then sums) in
   int per_split, nsplit;  // two launches: slabs a block, blocks a unit
+  long long slots;        // blocks that run at once
   size_t scores, stats, part, count, bytes;  // byte offsets in the workspace, and its size
 };
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -99,7 +100,7 @@ bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int s
   // at once and each has kMinSlabs; any number of blocks, not only powers of two (d = 128, 4 rows: 96 units of 8192 keys, 6
   // blocks a unit for 4: 43.8 -> 33.7 us; 192 of 2000, 3 for 2: 25.4 -> 20.4).  80 units of 600 keys with 8, 16 and 24
   // slabs at least: 11.5, 13.1 and 12.5 us; one slab a warp gains nothing more.
-  const long long slots = (long long)kSms * (a.nt == 2 && d == 128 ? 3 * kBlocksPerSm / 4 : kBlocksPerSm);
+  const long long slots = a.slots = (long long)kSms * (a.nt == 2 && d == 128 ? 3 * kBlocksPerSm / 4 : kBlocksPerSm);
   int c = (int)std::min<long long>((slabs + most - 1) / most, 8);
   a.shape = slabs <= c * std::min<long long>(2 * most, kBlockSlabs) ? SHAPE_CLUSTER : SHAPE_TWO;
   if (a.shape == SHAPE_CLUSTER) c = (int)std::max<long long>(c, std::min({8ll, slots / units, slabs / kMinSlabs}));
@@ -304,6 +305,7 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
   }
   p.G = a.G; p.tiles = a.tiles; p.nt = a.nt; p.max_slabs = a.max_slabs; p.slab_words = a.slab_words;
   p.wait_ns = serve_wait_ns();
+  p.sorted = 0;
   p.by_tiles = fast_div(a.tiles); p.by_kv = fast_div(cache->kv_heads); p.by_G = fast_div(a.G);
   const int vec = 4 * elem_size(dtype), qn = cache->d / 32, qvec = qn * elem_size(dtype);
   p.q_vec = reinterpret_cast<uintptr_t>(q->ptr) % qvec == 0 && q->stride_t % qn == 0 && q->stride_h % qn == 0;
@@ -319,6 +321,11 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
     p.per_split = 0;
     p.big_words = a.big_words;
     p.count = nullptr;
+    // More blocks than run at once: those of the longest requests first, so that the last ones to run are short (64 requests of
+    // 1021 to 8192 keys, 8 kv heads of 128: 97 -> 91 us; 32 of 1 to 8192: 56 -> 45).  Finding them costs a block 0.3 to 0.7 us, which
+    // lists under 32 slabs do not win back (120 requests of 1 to 300: 16.7 -> 17.4).  Where all lengths are near each other, 57 requests of 4096, the check costs 1%.
+    p.sorted = a.shape == SHAPE_CLUSTER && !window && B > 1 && B <= kMaxSorted && a.max_slabs >= 32 &&
+               (long long)B * cache->kv_heads * a.tiles * a.blocks > a.slots;
     if (a.shape == SHAPE_CLUSTER) return traced("k_attn", s, [&] { return launch(ATTN_ONE); });
     p.count = reinterpret_cast<int*>(ws + a.count);
     const int units = B * cache->kv_heads * a.tiles;

@@ -98,11 +98,37 @@ struct Unit {
   int nsink, wslab, n;     // slabs of the first tokens; the window's first slab; slabs in all
 };
 
-__device__ __forceinline__ Unit unit_of(const AttnP& p, int id, int cap, bool& bad) {
+// The request with the `rank`-th most tokens (ties: the first comes first), of at most kMaxSorted; `keys`: shared memory for
+// as many words.  Where no length is far from the first request's: the rank itself.  All of the block's threads; ends with a
+// barrier.
+__device__ __forceinline__ int request_of_rank(const AttnP& p, int rank, uint32_t* keys) {
+  static_assert(kThreads == kMaxSorted, "a request a thread");
+  __shared__ int who;
+  const int t = threadIdx.x;
+  auto length = [&](int b) { return min(max(__ldg(p.lens + b), 0), (1 << 24) - 1); };
+  const int len0 = length(0), len = t < p.B ? length(t) : len0;
+  if (!__syncthreads_or(abs(len - len0) > p.max_len >> 3)) return rank;
+  const uint32_t mine = t < p.B ? (uint32_t)(len + 1) << 7 | (uint32_t)(kMaxSorted - 1 - t) : 0u;  // distinct, and over those past B
+  keys[t] = mine;
+  if (t == 0) who = 0;
+  __syncthreads();
+  int before = 0;
+  for (int i = 0; i < p.B; i += 4) {
+    const uint4 x = *reinterpret_cast<const uint4*>(keys + i);
+    before += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+  }
+  if (t < p.B && before == rank) who = t;
+  __syncthreads();
+  return who;
+}
+
+// `keys`: shared memory for request_of_rank, or null: requests in their own order.
+__device__ __forceinline__ Unit unit_of(const AttnP& p, int id, int cap, bool& bad, uint32_t* keys = nullptr) {
   Unit u;
   const int head = quot(id, p.by_tiles), tile = id - head * p.tiles;
   u.b = quot(head, p.by_kv);
   u.h = head - u.b * p.c.kv;
+  if (keys && p.sorted) u.b = request_of_rank(p, u.b, keys);
   u.first = __ldg(p.cu + u.b);
   const int add = __ldg(p.cu + u.b + 1) - u.first, len = __ldg(p.lens + u.b);
   u.row0 = tile * cap;
@@ -974,7 +1000,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   pdl_wait();
   bool bad = false;
   const int C = p.nsplit, id = blockIdx.x / C, rank = blockIdx.x - id * C;
-  const Unit u = unit_of(p, id, R, bad);
+  const Unit u = unit_of(p, id, R, bad, reinterpret_cast<uint32_t*>(big));
   if (u.n == 0) {  // nothing to see, for every block of the cluster
     if (rank == 0) store_zeros(p, u, D);
     if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);

@@ -78,6 +78,7 @@ struct CacheIoP {
   unsigned* status;
 };
 
+constexpr int kMaxSorted = 128;
 struct AttnP {
   Heads q, o;
   Cache c;
@@ -97,6 +98,7 @@ struct AttnP {
   int* count;                        // one cooperative launch: [unit][2], zero before it; two launches: [unit]
   unsigned long long wait_ns;        // limit of a wait for the other blocks
   FastDiv by_tiles, by_kv, by_G;
+  int sorted;                        // one launch: the longest requests' blocks first (B <= kMaxSorted)
   int q_vec, o_vec;                  // d / 32 channels of a query row, four channels of the output in one access
   unsigned* status;
 };

@@ -148,6 +148,14 @@ def test_every_number_of_blocks_a_unit(blocks, heads, d, dtype):
     check_attention([128 * blocks + 5, 19, 0], [1, 1, 0], heads, 1, d, cfg, dtype, seed=17 + blocks)
 
 
+@pytest.mark.parametrize("requests", [110, 128, 129])
+@pytest.mark.parametrize("lo", [0, 600])
+def test_more_blocks_than_run_at_once(requests, lo):
+    """Many ragged requests (up to 128: the longest first) with equal lengths and empty ones among them, and nearly equal ones."""
+    lens = [lo + 50 * (i * 37 % 29 * (700 - lo) // 29 // 50) for i in range(requests)]
+    check_attention(lens, [min(n, 1) for n in lens], 6, 6, 64, kint.Config(Kint=4, calib=FWM, recon=LERP), BF16, seed=30)
+
+
 def test_many_tiles_with_long_lists():
     """Scores too many for shared memory: two launches, joined by the last block of each tile."""
     check_attention([8500], [150], 16, 1, 64, kint.Config(calib=SOFT), F32, block=256, seed=16)
