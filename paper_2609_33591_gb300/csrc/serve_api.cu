@@ -323,7 +323,8 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
     p.count = nullptr;
     // More blocks than run at once: those of the longest requests first, so that the last ones to run are short (64 requests of
     // 1021 to 8192 keys, 8 kv heads of 128: 97 -> 91 us; 32 of 1 to 8192: 56 -> 45).  Finding them costs a block 0.3 to 0.7 us, which
-    // lists under 32 slabs do not win back (120 requests of 1 to 300: 16.7 -> 17.4).  Where all lengths are near each other, 57 requests of 4096, the check costs 1%.
+    // lists under 32 slabs do not win back (120 requests of 1 to 300: 16.7 -> 17.4 us).  Where all lengths are near each other the check costs 1 to 2% (57 of 4096:
+    // 66.8 -> 68 us).
     p.sorted = a.shape == SHAPE_CLUSTER && !window && B > 1 && B <= kMaxSorted && a.max_slabs >= 32 &&
                (long long)B * cache->kv_heads * a.tiles * a.blocks > a.slots;
     if (a.shape == SHAPE_CLUSTER) return traced("k_attn", s, [&] { return launch(ATTN_ONE); });

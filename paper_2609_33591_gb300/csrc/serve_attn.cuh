@@ -39,8 +39,8 @@
 // Against that a block spends some 14000 cycles on what depends on one another (lengths, tables, first slabs, the exchange,
 // the join), which three other blocks on the SM cover in part; so small blocks of four warps, four a SM, do better than two
 // of eight (2048 units of 256 keys: 50 -> 35 us).  Measured on a GB300: 64 requests of 1021 to 8192 keys, 8 kv heads of 128,
-// bf16, FWM Nearest (347 MB) 100 us = 3.5 TB/s, 51% of the measured copy rate (a read of such slabs without arithmetic: 67 us
-// for 302 MB); one request of 131071 keys, MinMax (151 MB), cooperative, 43 us; four new tokens a request in windows of 1024
+// bf16, FWM Nearest (347 MB) 92 us = 3.8 TB/s, 56% of the measured copy rate (a read of such slabs without arithmetic: 67 us
+// for 302 MB); one request of 131071 keys, MinMax (151 MB), cooperative, 41 us; four new tokens a request in windows of 1024
 // keys (19 MB) 18 us; 8 requests of up to 1024 keys, 12 heads of 64, fp32 (4.3 MB) 9 us; one of 333 keys, 24 heads 5.8 us.
 #pragma once
 #include <atomic>

@@ -9,7 +9,7 @@
 // its slot, position and rotation are loaded once for all the heads it takes.  Several warps a token were slower on prompts
 // (one 137 us, six 205 us, in an earlier form of the loop below).
 // Measured on a GB300, 16381 tokens of 24 + 24 + 24 heads of 64 in bf16: append 62 us (interleaved rotation; 69 us half) for 229 MB
-// = 3.7 TB/s, bound by instruction issue (69% of the slots; some 170 instructions for 256 channels), read back 27 us for 129 MB =
+// = 3.7 TB/s, bound by instruction issue (70% of the slots; some 170 instructions for 256 channels), read back 27 us for 129 MB =
 // 4.8 TB/s; one step's 64 tokens 3.8 and 2.4 us.
 #include "serve_num.cuh"
 
