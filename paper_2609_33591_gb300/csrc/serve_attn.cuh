@@ -134,7 +134,8 @@ __device__ __forceinline__ Unit unit_of(const AttnP& p, int id, int cap, bool& b
   u.row0 = tile * cap;
   const bool there = u.first >= 0 && add >= 0 && u.first <= p.rows - add;  // its rows lie within q
   bad |= !there || add > p.max_new || len < 0 || len > p.max_len;
-  u.rows = there ? (int)min(max((long long)add * p.G - u.row0, 0ll), (long long)cap) : 0;
+  // (a request's rows past max_new are left out: the tiles, and what a tile keeps of its rows, are sized for max_new)
+  u.rows = there ? (int)min(max((long long)min(add, p.max_new) * p.G - u.row0, 0ll), (long long)cap) : 0;
   u.p0 = len - add;
   u.pmin = u.p0 + quot(u.row0, p.by_G);
   u.pmax = u.p0 + quot(u.row0 + max(u.rows, 1) - 1, p.by_G);
