@@ -136,9 +136,10 @@ __global__ void __launch_bounds__(kThreads) k_blocks(const BlocksP p) {
   if (base_a > (unsigned)p.tokens) bad = true;
   // blocks taken: the needs that fit, in order; the first request that finds too few ends it
   const int most = base_n < (unsigned)nfree ? (int)base_n : nfree;
-  const int gid = blockIdx.x * kThreads + threadIdx.x, gstep = gridDim.x * kThreads;
-  for (int k = gid; k < most; k += gstep) {
-    const int b = first_above(need, p.B, k);
+  // (unsigned: a step past the last of up to 2^31 - 1 places or blocks must not wrap to a negative index)
+  const unsigned gid = blockIdx.x * kThreads + threadIdx.x, gstep = gridDim.x * kThreads;
+  for (unsigned k1 = gid; k1 < (unsigned)most; k1 += gstep) {
+    const int k = (int)k1, b = first_above(need, p.B, k);
     if (need[b] > nfree) continue;
     const Req r = request(p, b, bad);
     const int first = need[b] - (r.want - r.held);
@@ -146,7 +147,8 @@ __global__ void __launch_bounds__(kThreads) k_blocks(const BlocksP p) {
   }
   // four consecutive tokens a thread: one bisection, one vector a result
   const int live = base_a < (unsigned)p.tokens ? (int)base_a : p.tokens;
-  for (int i0 = 4 * gid; i0 < p.tokens; i0 += 4 * gstep) {
+  for (unsigned at0 = 4 * gid; at0 < (unsigned)p.tokens; at0 += 4 * gstep) {
+    const int i0 = (int)at0, left = p.tokens - i0;
     int64_t slot[4];
     int pos[4], req[4];
     int q = i0 < live ? first_above(rows, p.B, i0) : p.B, have = -1, start = 0, n = 0;
@@ -156,8 +158,8 @@ __global__ void __launch_bounds__(kThreads) k_blocks(const BlocksP p) {
     for (int j = 0; j < 4; ++j) {
       slot[j] = -1;
       pos[j] = req[j] = -1;
+      if (live - i0 <= j) continue;
       const int i = i0 + j;
-      if (i >= live) continue;
       while (i >= rows[q]) ++q;
       if (q != have) {
         have = q;
@@ -179,7 +181,7 @@ __global__ void __launch_bounds__(kThreads) k_blocks(const BlocksP p) {
           bad = true;
       }
     }
-    if (p.vec && i0 + 4 <= p.tokens) {
+    if (p.vec && left >= 4) {
       reinterpret_cast<longlong2*>(p.slots + i0)[0] = make_longlong2(slot[0], slot[1]);
       reinterpret_cast<longlong2*>(p.slots + i0)[1] = make_longlong2(slot[2], slot[3]);
       *reinterpret_cast<int4*>(p.pos + i0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
@@ -187,7 +189,7 @@ __global__ void __launch_bounds__(kThreads) k_blocks(const BlocksP p) {
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (i0 + j < p.tokens) {
+        if (j < left) {
           p.slots[i0 + j] = slot[j];
           p.pos[i0 + j] = pos[j];
           p.req[i0 + j] = req[j];

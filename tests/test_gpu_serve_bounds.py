@@ -38,3 +38,18 @@ def test_rows_past_the_stated_bound_are_left_out(calib, heads, kv, bound, d, dty
     top = max(float(x.abs().max()) for x in pool.v if x.numel())
     bad = ((got - want).abs() > HALF_UNIT[dtype] * want.abs() + 3e-5 * top).any(-1) & safe
     assert not bad[at].any()
+
+
+def test_as_many_places_as_an_index_holds():
+    """2^31 - 1 places for 8 tokens (34 GB of slots, positions and requests)."""
+    tokens = (1 << 31) - 1
+    table = torch.full((2, 4), -1, dtype=torch.int32, device="cuda")
+    p = serve.extend_blocks(ints([0, 20]), ints([5, 3]), table, torch.arange(8, dtype=torch.int32, device="cuda"), ints([8]), 16, tokens)
+    # the second request's first two blocks are not in its table: its new tokens (places 20 to 22) have no slot
+    expect_flag()
+    assert p.slots[:10].tolist() == [112, 113, 114, 115, 116, -1, -1, -1, -1, -1]
+    assert p.pos[:10].tolist() == [0, 1, 2, 3, 4, 20, 21, 22, -1, -1] and p.req[:9].tolist() == [0] * 5 + [1] * 3 + [-1]
+    for x in (p.slots, p.pos, p.req):
+        for at in (1 << 30, 3 << 29, tokens - 700000):
+            assert (x[at:at + 700000] == -1).all()
+        assert (x[tokens - 9:] == -1).all()
