@@ -83,13 +83,14 @@ bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int s
     return false;
   a.G = q_heads / kv;
   const long long rows = (long long)max_new * a.G;
+  if (rows > (1 << 30)) return false;  // (a row's number is a 32-bit index, and so is a block's below)
   a.nt = rows <= 8 ? 1 : 2;
   const long long tiles = (rows + 8 * a.nt - 1) / (8 * a.nt);
   long long slabs = ((long long)max_len + 15) / 16;
   // keys from the window of a tile's first row to its last row, at any alignment, and the first tokens
   if (window) slabs = std::min(slabs, ((long long)sinks + 15) / 16 + ((long long)window + max_new) / 16 + 2);
+  if ((long long)B * kv > (1 << 30) / tiles) return false;
   const long long units = (long long)B * kv * tiles;
-  if (units > (1 << 30)) return false;
   a.tiles = (int)tiles;
   a.max_slabs = (int)slabs;
   a.slab_words = rows <= 4 ? 64 : 128 * a.nt;

@@ -139,7 +139,7 @@ __device__ __forceinline__ Unit unit_of(const AttnP& p, int id, int cap, bool& b
   u.p0 = len - add;
   u.pmin = u.p0 + quot(u.row0, p.by_G);
   u.pmax = u.p0 + quot(u.row0 + max(u.rows, 1) - 1, p.by_G);
-  u.low = p.window ? max(0, u.pmin - p.window + 1) : 0;
+  u.low = p.window ? max(0, max(u.pmin, 0) - p.window + 1) : 0;
   u.wslab = u.low >> 4;
   u.nsink = min((p.sinks + 15) >> 4, u.wslab);
   u.n = (u.rows > 0 && u.pmax >= 0) ? u.nsink + (u.pmax >> 4) - u.wslab + 1 : 0;
