@@ -145,6 +145,14 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
                     int table_stride, int width, const int32_t* lens, const int32_t* cu, int rows, int B, int window,
                     int sinks, int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
                     void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * kint_cache_attn for a step with places left over (kint_blocks_extend).  fill non-zero: rows of `out` that are no request's (before
+ * cu[0], from cu[B] on), and rows that are left out, get zeros; 0, as in kint_cache_attn: they are left as they are.
+ */
+int kint_cache_attn_step(const kint_heads* q, const kint_heads* out, const kint_cache* cache, const int32_t* table,
+                         int table_stride, int width, const int32_t* lens, const int32_t* cu, int rows, int B, int window,
+                         int sinks, int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
+                         int fill, void* workspace, size_t workspace_bytes, void* stream);
 size_t kint_cache_attn_workspace_bytes(int B, int q_heads, int kv_heads, int d, int window, int sinks, int max_new,
                                        int max_len);
 

@@ -270,6 +270,14 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
                     int table_stride, int width, const int32_t* lens, const int32_t* cu, int rows, int B, int window,
                     int sinks, int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
                     void* workspace, size_t workspace_bytes, void* stream) {
+  return kint_cache_attn_step(q, out, cache, table, table_stride, width, lens, cu, rows, B, window, sinks, Kint, calib, tau, recon, max_new,
+                              max_len, dtype, 0, workspace, workspace_bytes, stream);
+}
+
+int kint_cache_attn_step(const kint_heads* q, const kint_heads* out, const kint_cache* cache, const int32_t* table,
+                         int table_stride, int width, const int32_t* lens, const int32_t* cu, int rows, int B, int window,
+                         int sinks, int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
+                         int fill, void* workspace, size_t workspace_bytes, void* stream) {
   if (!valid_dtype(dtype) || !table || !lens || !cu || B < 1 || width < 1 || table_stride < width) return KINT_ERR_ARG;
   if (calib < 0 || calib > 5 || recon < 0 || recon > 1) return KINT_ERR_ARG;
   const bool grid = calib == KINT_CALIB_MINMAX || fwm_like(calib);
@@ -307,6 +315,7 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
   p.G = a.G; p.tiles = a.tiles; p.nt = a.nt; p.max_slabs = a.max_slabs; p.slab_words = a.slab_words;
   p.wait_ns = serve_wait_ns();
   p.sorted = 0;
+  p.fill = fill != 0;
   p.by_tiles = fast_div(a.tiles); p.by_kv = fast_div(cache->kv_heads); p.by_G = fast_div(a.G);
   const int vec = 4 * elem_size(dtype), qn = cache->d / 32, qvec = qn * elem_size(dtype);
   p.q_vec = reinterpret_cast<uintptr_t>(q->ptr) % qvec == 0 && q->stride_t % qn == 0 && q->stride_h % qn == 0;

@@ -321,6 +321,28 @@ __device__ __forceinline__ void store_o(const AttnP& p, long long off, const flo
     store_ch<__half, 4>(static_cast<__half*>(p.o.p) + off, p.o_vec, x);
 }
 
+// Rows of `out` that no unit answers, set to zero when the caller wants every row written (p.fill): those before the first
+// request's and behind the last one's (`ends`: cu[0], cu[B]), a row a block in turns; and, after an error in a request's
+// offsets or bound, its rows that are left out, by the first block of its first tile.
+__device__ __forceinline__ int2 row_ends(const AttnP& p) { return p.fill ? make_int2(__ldg(p.cu), __ldg(p.cu + p.B)) : make_int2(0, p.rows); }
+template <int D>
+__device__ __forceinline__ void zero_row(const AttnP& p, int row, int head, int heads) {
+  const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int x = threadIdx.x; x < heads * (D / 4); x += kThreads)
+    store_o(p, row * p.o.st + (head + x / (D / 4)) * p.o.sh + 4 * (x % (D / 4)), z);
+}
+template <int D>
+__device__ __forceinline__ void fill_rows(const AttnP& p, const Unit& u, int2 ends, bool bad, bool lead) {
+  const int from = min(max(ends.x, 0), p.rows), to = min(max(ends.y, 0), p.rows);
+  const long long rest = (long long)from + (p.rows - to);
+  for (long long r = blockIdx.x; r < rest; r += gridDim.x) zero_row<D>(p, (int)(r < from ? r : to + (r - from)), 0, p.o.n);
+  if (p.fill && bad && lead && u.row0 == 0) {
+    const int next = __ldg(p.cu + u.b + 1), add = next - u.first;
+    const bool there = u.first >= 0 && add >= 0 && u.first <= p.rows - add;
+    for (int r = there ? u.first + min(add, p.max_new) : max(u.first, 0); r < min(next, p.rows); ++r) zero_row<D>(p, r, u.h * p.G, p.G);
+  }
+}
+
 // Where a row of the tile lives.
 struct Row {
   int pos;         // its position; -1 past the tile's last row
@@ -1001,7 +1023,9 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   pdl_wait();
   bool bad = false;
   const int C = p.nsplit, id = blockIdx.x / C, rank = blockIdx.x - id * C;
+  const int2 ends = row_ends(p);
   const Unit u = unit_of(p, id, R, bad, reinterpret_cast<uint32_t*>(big));
+  fill_rows<D>(p, u, ends, bad, rank == 0);
   if (u.n == 0) {  // nothing to see, for every block of the cluster
     if (rank == 0) store_zeros(p, u, D);
     if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);
@@ -1183,7 +1207,9 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   pdl_wait();
   bool bad = false;
   const int id = blockIdx.x / p.nsplit, split = blockIdx.x - id * p.nsplit;
+  const int2 ends = row_ends(p);
   const Unit u = unit_of(p, id, R, bad);
+  fill_rows<D>(p, u, ends, bad, split == 0);
   const int i0 = split * p.per_split, i1 = min(i0 + p.per_split, u.n);
   const int active = (u.n + p.per_split - 1) / p.per_split;
   if (u.n == 0) {

@@ -23,7 +23,7 @@ struct Api {
   decltype(&kint_rope) rope;
   decltype(&kint_cache_append) append;
   decltype(&kint_cache_read) read;
-  decltype(&kint_cache_attn) attn;
+  decltype(&kint_cache_attn_step) attn;
   decltype(&kint_cache_attn_workspace_bytes) attn_ws;
 } api;
 PyObject* kint_error = nullptr;  // KintError(code, what)
@@ -355,7 +355,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         need(ws.is_cuda() && ws.is_contiguous(), "ws: expected a contiguous CUDA tensor");
       }
       run(api.attn(&hq, &ho, &c, pt, (int)table.stride(0), width, pl, pc, (int)q.size(0), B, window, sinks, whole(a[5]), (kint_calib)whole(a[6]),
-                   (float)tau, (kint_recon)whole(a[8]), max_new, max_len, type_of(q, "q"), ws.data_ptr(), ws.is_same(pages) ? kUnusedWorkspace : ws.nbytes(),
+                   (float)tau, (kint_recon)whole(a[8]), max_new, max_len, type_of(q, "q"), none(a[13]), ws.data_ptr(), ws.is_same(pages) ? kUnusedWorkspace : ws.nbytes(),
                    stream.handle),
           "kint_cache_attn");
     }

@@ -31,7 +31,7 @@ DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 # Every symbol include/kint_serve.h declares.
 EXPORTS = ("kint_cache_block_bytes", "kint_blocks_extend", "kint_rope_table", "kint_rope", "kint_cache_append",
-           "kint_cache_read", "kint_cache_attn", "kint_cache_attn_workspace_bytes")
+           "kint_cache_read", "kint_cache_attn", "kint_cache_attn_step", "kint_cache_attn_workspace_bytes")
 
 
 class kint_heads(ctypes.Structure):
@@ -62,6 +62,7 @@ def load():
                 ("kint_cache_append", [cp, hp, hp, vp, i, hp, hp, vp, vp, i, i, i, i, vp], i),
                 ("kint_cache_read", [cp, vp, i, hp, hp, i, vp], i),
                 ("kint_cache_attn", [hp, hp, cp, vp, i, i, vp, vp, i, i, i, i, i, i, f, i, i, i, i, vp, sz, vp], i),
+                ("kint_cache_attn_step", [hp, hp, cp, vp, i, i, vp, vp, i, i, i, i, i, i, f, i, i, i, i, i, vp, sz, vp], i),
                 ("kint_cache_attn_workspace_bytes", [i] * 8, sz)):
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, res
@@ -81,7 +82,7 @@ def _ext():
         mod = importlib.util.module_from_spec(importlib.util.spec_from_loader("_kint_serve", loader))
         loader.exec_module(mod)
         mod.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
-            "kint_blocks_extend", "kint_rope", "kint_cache_append", "kint_cache_read", "kint_cache_attn",
+            "kint_blocks_extend", "kint_rope", "kint_cache_append", "kint_cache_read", "kint_cache_attn_step",
             "kint_cache_attn_workspace_bytes")), kint.KintError)
         _mod = mod
     return _mod
@@ -210,7 +211,8 @@ def attention(q, pages, table, lens, cu, cfg: kint.Config, *, window: int = 0, s
     """K-interval attention of new tokens over the cache: q [rows, heads, d], request b's rows cu[b] .. cu[b + 1] - 1 at
     the last positions of its lens[b] cached tokens, whose blocks are table[b].  window > 0: a row sees its last
     ``window`` keys and the first ``sinks``.  max_new and max_len bound the rows a request has and lens (host numbers
-    that size the launch; by default rows and what the table can hold)."""
+    that size the launch; by default rows and what the table can hold).  Rows that are no request's, or left out for
+    their bounds, are zero in a new output and left as they are in ``out``."""
     return (_mod or _ext()).attention(q, pages, table, lens, cu, cfg.Kint, cfg.calib, cfg.tau, cfg.recon, window, sinks, max_new,
                                       max_len, out, ws, _handle(stream))
 

@@ -53,3 +53,68 @@ def test_as_many_places_as_an_index_holds():
         for at in (1 << 30, 3 << 29, tokens - 700000):
             assert (x[at:at + 700000] == -1).all()
         assert (x[tokens - 9:] == -1).all()
+
+
+# the three ways in which attention is launched: lengths, heads of one kv head
+WAYS = [([40, 3, 0, 300], 4), ([40, 3, 0, 300], 16), ([9000, 3, 0, 30], 4), ([8300, 3, 0, 30], 8)]
+
+
+def poison(like):
+    """Freed memory full of NaN, which an output of the same size is given next."""
+    torch.cuda.synchronize()
+    x = torch.full_like(like, float("nan"))
+    torch.cuda.synchronize()
+    del x
+
+
+@pytest.mark.parametrize("before,behind", [(0, 5), (3, 0), (2, 700)])
+@pytest.mark.parametrize("lens,heads", WAYS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_of_no_request_are_zero(dtype, lens, heads, before, behind):
+    """Rows of q before the first request's and behind the last one's; in a given `out` they are left as they are."""
+    max_new = 130 if heads == 8 else 2
+    new = [min(n, e) for n, e in zip(lens, (max_new, 1, 0, 2))]
+    pool = filled(lens, 1, 64, 64, 60)
+    q = torch.randn(before + sum(new) + behind, heads, 64, device="cuda").to(dtype)
+    cu = ints([before + x for x in offsets(new)])
+    args, kw = (gpu(pool.pages), gpu(pool.table), gpu(pool.lens)), dict(max_new=max_new)
+    cfg, inner = kint.Config(calib=FWM, recon=LERP), slice(before, before + sum(new))
+    want = serve.attention(q[inner].contiguous(), *args, ints(offsets(new)), cfg, **kw)
+    poison(q)
+    got = serve.attention(q, *args, cu, cfg, **kw)
+    assert torch.equal(got[inner], want)
+    assert (got[:before] == 0).all() and (got[inner.stop:] == 0).all()
+    out = torch.full_like(q, 7.0)
+    serve.attention(q, *args, cu, cfg, out=out, **kw)
+    assert torch.equal(out[inner], want) and (out[:before] == 7.0).all() and (out[inner.stop:] == 7.0).all()
+
+
+@pytest.mark.parametrize("cu", [[-1, 0], [0, 2], [1, 2], [3, 2]])
+def test_rows_that_q_does_not_have_leave_zeros(cu):
+    """A request left out for its offsets: flagged, and a new output holds zeros."""
+    pool = filled([40], 2, 64, 32, 14)
+    q = torch.randn(1, 2, 64, device="cuda")
+    poison(q)
+    o = serve.attention(q, gpu(pool.pages), gpu(pool.table), gpu(pool.lens), ints(cu), kint.Config(calib=SOFT), max_new=4)
+    expect_flag()
+    assert (o == 0).all()
+
+
+def test_rows_past_the_stated_bound_are_zero_in_a_new_output():
+    pool = filled([40], 2, 64, 32, 14)
+    q = torch.randn(9, 4, 64, device="cuda")
+    poison(q)
+    o = serve.attention(q, gpu(pool.pages), gpu(pool.table), gpu(pool.lens), ints([0, 9]), kint.Config(calib=SOFT), max_new=2)
+    expect_flag()
+    assert (o[:2] != 0).any() and (o[2:] == 0).all()
+
+
+def test_a_step_with_places_left_over():
+    """Places behind the last new token go through the layer as rows of zeros, not as what memory holds."""
+    layer = serve.KIntServingAttention(256, 4, kint.Config(calib=FWM), max_pos=128)
+    cache = serve.PagedCache(1, 2, 128, 16, 4, 64, block_size=16)
+    x = torch.randn(9, 256, device="cuda")
+    plan = cache.extend(ints([3, 2]), 9)
+    poison(torch.empty(9, 4, 64, device="cuda"))
+    y = layer.step(x, cache, plan, max_new=3)
+    assert torch.isfinite(y).all() and torch.equal(y[5:], layer.c_proj(torch.zeros(4, 256, device="cuda")).detach())
