@@ -83,7 +83,8 @@ size_t kint_cache_block_bytes(int block_size, int kv_heads, int d);
  *             token; places past cu[B] get -1.  Tokens past `tokens` places are not written, and flagged.
  *   refused   out [1] int32: requests that got no blocks: their row of the table is too short, or the
  *             free blocks ran out (requests are served in order; from the first that finds too few,
- *             every one that needs a block is refused).  Their slots are -1 and their length stays.
+ *             every one that needs a block is refused).  Their slots are -1 and their length stays, but cu counts their
+ *             tokens: hand the slots to kint_cache_attn_step, which answers them with zeros.
  * The outputs must not overlap the inputs (table apart), so the call can be repeated.  1 <= B <= 16384.
  */
 int kint_blocks_extend(const int32_t* lens, const int32_t* add, int32_t* table, int table_stride, int width,
@@ -146,13 +147,17 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
                     int sinks, int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
                     void* workspace, size_t workspace_bytes, void* stream);
 /*
- * kint_cache_attn for a step with places left over (kint_blocks_extend).  fill non-zero: rows of `out` that are no request's (before
- * cu[0], from cu[B] on), and rows that are left out, get zeros; 0, as in kint_cache_attn: they are left as they are.
+ * kint_cache_attn for a step as kint_blocks_extend plans it, with places left over and requests refused:
+ *   slots  [rows] int64, the slots of q's rows, or NULL.  A request whose first new token has none (-1) was refused: its new
+ *          tokens are not in the cache, lens[b] does not count them, and its rows give zeros.  Without slots they are taken for
+ *          the last lens[b] positions, which hold older tokens.
+ *   fill   non-zero: rows of `out` that are no request's (before cu[0], from cu[B] on), and rows that are left out, get zeros; 0, as
+ *          in kint_cache_attn: they are left as they are.
  */
 int kint_cache_attn_step(const kint_heads* q, const kint_heads* out, const kint_cache* cache, const int32_t* table,
                          int table_stride, int width, const int32_t* lens, const int32_t* cu, int rows, int B, int window,
                          int sinks, int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
-                         int fill, void* workspace, size_t workspace_bytes, void* stream);
+                         const int64_t* slots, int fill, void* workspace, size_t workspace_bytes, void* stream);
 size_t kint_cache_attn_workspace_bytes(int B, int q_heads, int kv_heads, int d, int window, int sinks, int max_new,
                                        int max_len);
 

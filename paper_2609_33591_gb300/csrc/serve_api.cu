@@ -271,13 +271,13 @@ int kint_cache_attn(const kint_heads* q, const kint_heads* out, const kint_cache
                     int sinks, int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
                     void* workspace, size_t workspace_bytes, void* stream) {
   return kint_cache_attn_step(q, out, cache, table, table_stride, width, lens, cu, rows, B, window, sinks, Kint, calib, tau, recon, max_new,
-                              max_len, dtype, 0, workspace, workspace_bytes, stream);
+                              max_len, dtype, nullptr, 0, workspace, workspace_bytes, stream);
 }
 
 int kint_cache_attn_step(const kint_heads* q, const kint_heads* out, const kint_cache* cache, const int32_t* table,
                          int table_stride, int width, const int32_t* lens, const int32_t* cu, int rows, int B, int window,
                          int sinks, int Kint, kint_calib calib, float tau, kint_recon recon, int max_new, int max_len, kint_dtype dtype,
-                         int fill, void* workspace, size_t workspace_bytes, void* stream) {
+                         const int64_t* slots, int fill, void* workspace, size_t workspace_bytes, void* stream) {
   if (!valid_dtype(dtype) || !table || !lens || !cu || B < 1 || width < 1 || table_stride < width) return KINT_ERR_ARG;
   if (calib < 0 || calib > 5 || recon < 0 || recon > 1) return KINT_ERR_ARG;
   const bool grid = calib == KINT_CALIB_MINMAX || fwm_like(calib);
@@ -292,6 +292,7 @@ int kint_cache_attn_step(const kint_heads* q, const kint_heads* out, const kint_
   if (max_len > (1 << 30) || max_new > (1 << 24) || q->heads > (1 << 16)) return KINT_ERR_UNSUPPORTED;
   for (const void* x : {(const void*)table, (const void*)lens, (const void*)cu})
     if (reinterpret_cast<uintptr_t>(x) % 4) return KINT_ERR_ALIGN;
+  if (reinterpret_cast<uintptr_t>(slots) % 8) return KINT_ERR_ALIGN;
   AttnPlan a;
   if (!plan_attn(a, B, q->heads, cache->kv_heads, cache->d, window, sinks, max_new, max_len)) return KINT_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < a.bytes) return KINT_ERR_WORKSPACE;
@@ -316,6 +317,7 @@ int kint_cache_attn_step(const kint_heads* q, const kint_heads* out, const kint_
   p.wait_ns = serve_wait_ns();
   p.sorted = 0;
   p.fill = fill != 0;
+  p.slots = slots;
   p.by_tiles = fast_div(a.tiles); p.by_kv = fast_div(cache->kv_heads); p.by_G = fast_div(a.G);
   const int vec = 4 * elem_size(dtype), qn = cache->d / 32, qvec = qn * elem_size(dtype);
   p.q_vec = reinterpret_cast<uintptr_t>(q->ptr) % qvec == 0 && q->stride_t % qn == 0 && q->stride_h % qn == 0;

@@ -143,6 +143,8 @@ __device__ __forceinline__ Unit unit_of(const AttnP& p, int id, int cap, bool& b
   u.wslab = u.low >> 4;
   u.nsink = min((p.sinks + 15) >> 4, u.wslab);
   u.n = (u.rows > 0 && u.pmax >= 0) ? u.nsink + (u.pmax >> 4) - u.wslab + 1 : 0;
+  // refused (kint_blocks_extend): its new tokens are not in the cache and its length does not count them
+  if (p.slots && u.rows > 0 && __ldg(p.slots + u.first) < 0) u.n = 0;
   if (u.n > p.max_slabs) {
     bad = true;
     u.n = p.max_slabs;

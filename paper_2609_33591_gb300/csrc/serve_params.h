@@ -99,6 +99,7 @@ struct AttnP {
   unsigned long long wait_ns;        // limit of a wait for the other blocks
   FastDiv by_tiles, by_kv, by_G;
   int sorted;                        // one launch: the longest requests' blocks first (B <= kMaxSorted)
+  const int64_t* slots;              // slots of q's rows, or null: a request whose first has none gets zeros
   int fill;                          // rows of the output that no request answers get zeros
   int q_vec, o_vec;                  // d / 32 channels of a query row, four channels of the output in one access
   unsigned* status;

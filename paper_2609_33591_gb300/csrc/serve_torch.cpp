@@ -320,9 +320,9 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// q, pages, table, lens, cu, Kint, calib, tau, recon, window, sinks, max_new, max_len, out, ws, stream -> out
+// q, pages, table, lens, cu, Kint, calib, tau, recon, window, sinks, max_new, max_len, out, ws, slots, stream -> out
 PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 16, [&]() -> PyObject* {
+  return guarded(n, 17, [&]() -> PyObject* {
     const at::Tensor &q = tensor(a[0], "q"), &pages = tensor(a[1], "pages"), &table = tensor(a[2], "table"), &lens = tensor(a[3], "lens"),
                      &cu = tensor(a[4], "cu");
     const kint_heads hq = heads(q, "q", 3);
@@ -337,7 +337,13 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int max_len = none(a[12]) ? (int)(hold < INT32_MAX ? hold : INT32_MAX) : whole(a[12]);
     const double tau = PyFloat_AsDouble(a[7]);
     if (tau == -1.0 && PyErr_Occurred()) throw Refused();
-    const CallStream stream(a[15]);
+    const int64_t* slots = nullptr;
+    if (!none(a[15])) {
+      const at::Tensor& t = tensor(a[15], "slots");
+      need(t.dim() == 1 && t.size(0) == q.size(0), "slots: expected one for each row of q");
+      slots = ints<int64_t>(t, "slots");
+    }
+    const CallStream stream(a[16]);
     at::Tensor out = none(a[13]) ? at::empty_like(q) : tensor(a[13], "out");
     need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out disagrees with q");
     if (q.numel()) {
@@ -355,7 +361,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         need(ws.is_cuda() && ws.is_contiguous(), "ws: expected a contiguous CUDA tensor");
       }
       run(api.attn(&hq, &ho, &c, pt, (int)table.stride(0), width, pl, pc, (int)q.size(0), B, window, sinks, whole(a[5]), (kint_calib)whole(a[6]),
-                   (float)tau, (kint_recon)whole(a[8]), max_new, max_len, type_of(q, "q"), none(a[13]), ws.data_ptr(), ws.is_same(pages) ? kUnusedWorkspace : ws.nbytes(),
+                   (float)tau, (kint_recon)whole(a[8]), max_new, max_len, type_of(q, "q"), slots, none(a[13]), ws.data_ptr(), ws.is_same(pages) ? kUnusedWorkspace : ws.nbytes(),
                    stream.handle),
           "kint_cache_attn");
     }

@@ -6,7 +6,7 @@ given, to which the memory that a call allocates then belongs.  One step of a la
 
     plan = extend_blocks(...)                       # once a step
     q = append(k, v, plan.slots, pages, q=q, pos=plan.pos, table=rope)
-    o = attention(q, pages, blocks, plan.lens, plan.cu, cfg, ...)
+    o = attention(q, pages, blocks, plan.lens, plan.cu, cfg, slots=plan.slots, ...)
 
 ``PagedCache`` keeps the tables and lengths between steps, ``rotary`` is the differentiable
 rotation for training, and ``KIntServingAttention`` is the GPT-2 block of ``attention`` with
@@ -62,7 +62,7 @@ def load():
                 ("kint_cache_append", [cp, hp, hp, vp, i, hp, hp, vp, vp, i, i, i, i, vp], i),
                 ("kint_cache_read", [cp, vp, i, hp, hp, i, vp], i),
                 ("kint_cache_attn", [hp, hp, cp, vp, i, i, vp, vp, i, i, i, i, i, i, f, i, i, i, i, vp, sz, vp], i),
-                ("kint_cache_attn_step", [hp, hp, cp, vp, i, i, vp, vp, i, i, i, i, i, i, f, i, i, i, i, i, vp, sz, vp], i),
+                ("kint_cache_attn_step", [hp, hp, cp, vp, i, i, vp, vp, i, i, i, i, i, i, f, i, i, i, i, vp, i, vp, sz, vp], i),
                 ("kint_cache_attn_workspace_bytes", [i] * 8, sz)):
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, res
@@ -207,14 +207,15 @@ def read(pages, slots, *, dtype=torch.float32, stream=None):
 
 
 def attention(q, pages, table, lens, cu, cfg: kint.Config, *, window: int = 0, sinks: int = 0, max_new: int | None = None,
-              max_len: int | None = None, out=None, ws=None, stream=None):
+              max_len: int | None = None, slots=None, out=None, ws=None, stream=None):
     """K-interval attention of new tokens over the cache: q [rows, heads, d], request b's rows cu[b] .. cu[b + 1] - 1 at
     the last positions of its lens[b] cached tokens, whose blocks are table[b].  window > 0: a row sees its last
     ``window`` keys and the first ``sinks``.  max_new and max_len bound the rows a request has and lens (host numbers
-    that size the launch; by default rows and what the table can hold).  Rows that are no request's, or left out for
+    that size the launch; by default rows and what the table can hold).  ``slots``: the plan's, so that requests it refused
+    get zeros (without them their rows are taken for the last positions of what is cached).  Rows that are no request's, or left out for
     their bounds, are zero in a new output and left as they are in ``out``."""
     return (_mod or _ext()).attention(q, pages, table, lens, cu, cfg.Kint, cfg.calib, cfg.tau, cfg.recon, window, sinks, max_new,
-                                      max_len, out, ws, _handle(stream))
+                                      max_len, out, ws, slots, _handle(stream))
 
 
 def attention_workspace(B: int, heads: int, kv_heads: int, d: int, *, window: int = 0, sinks: int = 0, max_new: int = 1,
@@ -284,12 +285,13 @@ class KIntServingAttention(KIntSelfAttention):
     @torch.no_grad()
     def step(self, x, cache: PagedCache, plan: BlockPlan, layer: int = 0, *, max_new: int | None = None,
              max_len: int | None = None):
-        """x [rows, C]: the new tokens of every request in the plan's order (cache.extend)."""
+        """x [rows, C]: the new tokens of every request in the plan's order (cache.extend).  Places left over and requests that
+        the plan refused get the projection of zeros."""
         rows, C = x.shape
         D = C // self.n_head
         q, k, v = (t.view(rows, self.n_head, D) for t in self.c_attn(x).split(C, dim=1))
         pages = cache.pages[layer]
         q = append(k, v, plan.slots, pages, q=q, pos=plan.pos, table=self.rope, interleaved=self.interleaved)
         y = attention(q, pages, cache.table, plan.lens, plan.cu, self.cfg, window=self.window, sinks=self.sinks,
-                      max_new=max_new, max_len=max_len or cache.max_len)
+                      max_new=max_new, max_len=max_len or cache.max_len, slots=plan.slots)
         return self.c_proj(y.view(rows, C))

@@ -118,3 +118,48 @@ def test_a_step_with_places_left_over():
     poison(torch.empty(9, 4, 64, device="cuda"))
     y = layer.step(x, cache, plan, max_new=3)
     assert torch.isfinite(y).all() and torch.equal(y[5:], layer.c_proj(torch.zeros(4, 256, device="cuda")).detach())
+
+
+@pytest.mark.parametrize("lens,heads", WAYS)
+def test_refused_requests_get_zeros(lens, heads):
+    """With the plan's slots, rows of a request that found no blocks are zero (their keys are not in the cache); the others'
+    bits do not change.  Through a given `out` too."""
+    max_new = 130 if heads == 8 else 2
+    new = [min(n, e) for n, e in zip(lens, (max_new, 1, 0, 2))]
+    pool = filled(lens, 1, 64, 64, 61)
+    q = torch.randn(sum(new) + 2, heads, 64, device="cuda")
+    args = gpu(pool.pages), gpu(pool.table), gpu(pool.lens), ints(offsets(new)), kint.Config(calib=FWM, recon=LERP)
+    want = serve.attention(q, *args, max_new=max_new)
+    for b in (0, 1, 3):
+        slots = torch.arange(q.size(0), device="cuda")
+        rows = slice(sum(new[:b]), sum(new[:b + 1]))
+        slots[rows] = -1
+        slots[sum(new):] = -1
+        for out in (None, torch.full_like(q, 7.0)):
+            poison(q)
+            got = serve.attention(q, *args, max_new=max_new, slots=slots, out=out)
+            assert (got[rows] == 0).all() and torch.equal(got[:rows.start], want[:rows.start])
+            assert torch.equal(got[rows.stop:sum(new)], want[rows.stop:sum(new)])
+            assert (got[sum(new):] == (0.0 if out is None else 7.0)).all()
+
+
+def test_a_step_that_refuses_a_request():
+    """Two blocks of 16 for two requests of 16 and 10 tokens: the third is refused, and later the first finds no block for its
+    17th.  Their rows are the projection of zeros; the others' are what they are without them."""
+    torch.manual_seed(2)
+    layer = serve.KIntServingAttention(256, 4, kint.Config(calib=FWM), max_pos=64)
+    cache, twin = (serve.PagedCache(1, 3, 64, n, 4, 64, block_size=16) for n in (2, 8))
+    zero = layer.c_proj(torch.zeros(1, 256, device="cuda")).detach()
+    x = torch.randn(33, 256, device="cuda")
+    y = layer.step(x, cache, cache.extend(ints([16, 10, 7]), 33), max_new=16)
+    z = layer.step(x, twin, twin.extend(ints([16, 10, 7]), 33), max_new=16)
+    assert torch.equal(y[:26], z[:26]) and torch.equal(y[26:], zero.expand(7, -1)) and not torch.equal(z[26:], y[26:])
+    x = torch.randn(2, 256, device="cuda")
+    plan = cache.extend(ints([1, 1, 0]), 2)
+    y = layer.step(x, cache, plan, max_new=1)
+    z = layer.step(x, twin, twin.extend(ints([1, 1, 0]), 2), max_new=1)
+    assert int(plan.refused) == 1 and cache.lens.tolist() == [16, 11, 0]
+    assert torch.equal(y[:1], zero) and torch.equal(y[1], z[1])
+    with pytest.raises(ValueError):
+        serve.attention(torch.zeros(2, 4, 64, device="cuda"), cache.pages[0], cache.table, plan.lens, plan.cu, kint.Config(),
+                        slots=plan.slots[:1])
