@@ -210,8 +210,10 @@ __global__ void __launch_bounds__(kThreads) k_blocks(const BlocksP p) {
 
 cudaError_t launch_blocks(const BlocksP& p, int nsm, cudaStream_t s) {
   const int smem = 2 * p.B * (int)sizeof(int);
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(k_blocks, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  // The limit without asking, 48 KB, holds the kernel's static shared memory too; so ask well below it, and for the largest call's
+  // bytes, so that a call in another host thread never finds them taken back.
+  if (smem > 32 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(k_blocks, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxRequests * (int)sizeof(int));
     if (e != cudaSuccess) return e;
   }
   // 4 tokens a thread, and no more CTAs than run at once (each forms the prefix sums again)

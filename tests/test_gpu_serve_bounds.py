@@ -1,5 +1,7 @@
 """GPU: what the serving operators do at and past the bounds that a caller states, and with rows, blocks and memory that
 belong to nobody.  Tolerances are those of test_gpu_serve.py; the rest is equality."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -14,6 +16,42 @@ pytestmark = pytest.mark.gpu
 
 def offsets(new):
     return np.concatenate([[0], np.cumsum(new)]).tolist()
+
+
+@pytest.mark.parametrize("requests", [6110, 6111, 6144, 6145, 16384, 6111])
+def test_blocks_of_many_requests(requests):
+    """Prefix sums at and past 48 KB of shared memory (6111 to 6144 requests reach it with what the kernel holds besides), up to
+    the largest number of requests."""
+    from tests.test_gpu_serve import check_blocks
+    rng = np.random.default_rng(requests)
+    lens, new = rng.integers(0, 60, requests).tolist(), rng.integers(0, 4, requests).tolist()
+    check_blocks(lens, new, 4, 16, requests, sum(new) + 3, seed=requests)
+
+
+def test_blocks_from_several_host_threads():
+    """Calls of very different sizes at once: no thread's shared memory is taken back by another's."""
+    rcs = []
+
+    def work(requests):
+        i32 = dict(dtype=torch.int32, device="cuda")
+        lens, new = torch.zeros(requests, **i32), torch.ones(requests, **i32)
+        table, free, n_free = torch.zeros(requests, 1, **i32), torch.arange(requests, **i32), ints([requests])
+        out = torch.empty(8 * requests + 8, **i32)
+        slots = torch.empty(requests, dtype=torch.int64, device="cuda")
+        at = [x.data_ptr() for x in (out, out[8 * requests:], out[2 * requests:], slots, out[4 * requests:], out[5 * requests:],
+                                     out[8 * requests + 4:])]
+        torch.cuda.synchronize()
+        for _ in range(300):
+            rcs.append(serve.load().kint_blocks_extend(lens.data_ptr(), new.data_ptr(), table.data_ptr(), 1, 1, free.data_ptr(), requests,
+                                                       n_free.data_ptr(), requests, 16, requests, *at, None))
+
+    threads = [threading.Thread(target=work, args=(n,)) for n in (16384, 7000, 12000, 9000)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert len(rcs) == 1200 and not any(rcs)
 
 
 @pytest.mark.parametrize("calib", [SOFT, FWM, MM])
