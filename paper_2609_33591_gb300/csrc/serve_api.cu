@@ -72,7 +72,6 @@ struct AttnPlan {
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 constexpr int kSms = 152;
 constexpr int kBlocksPerSm = 16 / kAttnWarps;          // of at most 128 registers a thread
-constexpr int kScoreWords = 8192;                      // 32 KB of scores a block, beside 20 KB of copies in flight
 constexpr int kBlockSlabs = 32 * kAttnWarps;           // a warp keeps the addresses of 32
 constexpr int kMinSlabs = 2 * kAttnWarps;              // fewest slabs a block that splitting a unit over a cluster leaves
 constexpr int kMinCoop = 8 * kAttnWarps;               // and over a cooperative launch
@@ -103,7 +102,7 @@ bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int s
   // slabs at least: 11.5, 13.1 and 12.5 us; one slab a warp gains nothing more.
   const long long slots = a.slots = (long long)kSms * (a.nt == 2 && d == 128 ? 3 * kBlocksPerSm / 4 : kBlocksPerSm);
   int c = (int)std::min<long long>((slabs + most - 1) / most, 8);
-  a.shape = slabs <= c * std::min<long long>(2 * most, kBlockSlabs) ? SHAPE_CLUSTER : SHAPE_TWO;
+  a.shape = slabs <= c * std::min<long long>(kMaxScoreWords / a.slab_words, kBlockSlabs) ? SHAPE_CLUSTER : SHAPE_TWO;
   if (a.shape == SHAPE_CLUSTER) c = (int)std::max<long long>(c, std::min({8ll, slots / units, slabs / kMinSlabs}));
   // Where the units are so few that twice those blocks and more run at once, a cooperative launch.  (Its exchange is dearer:
   // 64 units of 8192 keys take 31.0 us with 9 blocks a unit so, 26.6 as clusters of 8; 16 slabs a block at least: 32 units

@@ -53,6 +53,7 @@
 namespace kint {
 namespace {
 
+static_assert(kMaxScoreWords >= kAttnWarps * 16 * 128, "partial sums lie where the scores were");
 constexpr int kWarps = kAttnWarps, kThreads = 32 * kWarps;
 constexpr int kMaxGranted = 64;  // devices whose shared-memory grants are remembered
 constexpr float kMasked = -1.0e38f;   // score of a (row, key) that is not visible; a weight of 0 in every form
@@ -1282,38 +1283,41 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
 
 // ---- launches --------------------------------------------------------------------------------------------
 
-// Lets a kernel use `bytes` of dynamic shared memory on the current device; asked of the runtime once a size.
+// Lets a kernel use up to `most` bytes of dynamic shared memory on the current device, asked of the runtime once.  The same
+// number from every call, so that host threads that ask at once cannot take each other's back.
 template <class Kern>
-cudaError_t want_smem(Kern kern, int bytes, std::atomic<int> (&granted)[kMaxGranted]) {
+cudaError_t want_smem(Kern kern, int bytes, int most, std::atomic<bool> (&granted)[kMaxGranted]) {
+  if (bytes > most) return cudaErrorInvalidValue;
   int dev = 0;
   if (cudaError_t e = cudaGetDevice(&dev)) return e;
   const bool known = dev >= 0 && dev < kMaxGranted;
-  if (bytes <= 32 * 1024 || (known && granted[dev].load(std::memory_order_relaxed) >= bytes)) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess && known) granted[dev].store(bytes, std::memory_order_relaxed);
+  if (known && granted[dev].load(std::memory_order_relaxed)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+  if (e == cudaSuccess && known) granted[dev].store(true, std::memory_order_relaxed);
   return e;
 }
 
 template <int D, int NT, bool FOUR, bool F32, int MODE>
 cudaError_t go(const AttnP& p, int what, int grid, cudaStream_t s) {
   const int tab = MODE == M_GRID ? (p.calib == CAL_MINMAX ? 8 * NT : 1) * table_len(p.Kint) * (int)sizeof(float2) : 0;
+  constexpr int kSums = kWarps * 8 * NT * D * (int)sizeof(float), kTab = MODE == M_GRID ? 8 * NT * table_len(KMAX) * (int)sizeof(float2) : 0;
   if (what == ATTN_ONE) {
     const int smem = Ring<D>::kBytes + p.big_words * 4 + tab;
-    static std::atomic<int> granted[kMaxGranted];
-    if (cudaError_t e = want_smem(k_attn<D, NT, FOUR, F32, MODE>, smem, granted)) return e;
+    static std::atomic<bool> granted[kMaxGranted];
+    if (cudaError_t e = want_smem(k_attn<D, NT, FOUR, F32, MODE>, smem, Ring<D>::kBytes + kMaxScoreWords * 4 + kTab, granted)) return e;
     if (p.count) return launch_cooperative(k_attn<D, NT, FOUR, F32, MODE>, dim3(grid), dim3(kThreads), smem, s, p);
     return launch_pdl_cluster(k_attn<D, NT, FOUR, F32, MODE>, dim3(grid), dim3(kThreads), smem, p.nsplit, s, p);
   }
-  const int smem = Ring<D>::kBytes + kWarps * 8 * NT * D * (int)sizeof(float) + tab;
-  static std::atomic<int> granted[kMaxGranted];
-  if (cudaError_t e = want_smem(k_attn_values<D, NT, FOUR, F32, MODE>, smem, granted)) return e;
+  const int smem = Ring<D>::kBytes + kSums + tab;
+  static std::atomic<bool> granted[kMaxGranted];
+  if (cudaError_t e = want_smem(k_attn_values<D, NT, FOUR, F32, MODE>, smem, Ring<D>::kBytes + kSums + kTab, granted)) return e;
   return launch_pdl(k_attn_values<D, NT, FOUR, F32, MODE>, dim3(grid), dim3(kThreads), smem, s, p);
 }
 template <int D, int NT, bool F32, bool LOW>
 cudaError_t go_scores(const AttnP& p, int grid, cudaStream_t s) {
-  static std::atomic<int> granted[kMaxGranted];
+  static std::atomic<bool> granted[kMaxGranted];
   constexpr int smem = Ring<D>::kBytes + QTile<D, NT, F32>::kBytes;
-  if (cudaError_t e = want_smem(k_attn_scores<D, NT, F32, LOW>, smem, granted)) return e;
+  if (cudaError_t e = want_smem(k_attn_scores<D, NT, F32, LOW>, smem, smem, granted)) return e;
   return launch_pdl(k_attn_scores<D, NT, F32, LOW>, dim3(grid), dim3(kThreads), smem, s, p);
 }
 template <int D, int NT, bool FOUR, bool F32>

@@ -9,6 +9,8 @@ namespace kint {
 
 constexpr int kMaxRequests = 16384;  // requests of one kint_blocks_extend: two 32-bit prefix sums each in shared memory
 constexpr int kAttnWarps = 4;        // warps of an attention block
+constexpr int kScoreWords = 8192;    // scores a block of it keeps: 32 KB, beside 20 KB of copies in flight, so that four fit an SM
+constexpr int kMaxScoreWords = 2 * kScoreWords;  // and at most
 constexpr int kGroup = 64;           // channels that share one (scale, centre) pair of the cache
 
 enum Dtype : int { DT_FP32 = 0, DT_BF16 = 1, DT_FP16 = 2 };
