@@ -121,7 +121,7 @@ bool plan_attn(AttnPlan& a, int B, int q_heads, int kv, int d, int window, int s
     return units * c <= 0x7fffffffll;
   }
   // Two launches: 128 slabs a block (64: 240 units of 30000 keys 337 us, 128: 313), fewer while the grid is under two blocks a
-  // SM, 8 at least.  (A cooperative launch that the device has no room for runs so too.)
+  // SM, 8 at least.  (A cooperative launch that the device has no room for at once runs so too.)
   long long per = 128;
   while (per > 8 && units * ((slabs + per - 1) / per) < 2 * kSms) per >>= 1;
   const long long nsplit = (slabs + per - 1) / per;
@@ -339,13 +339,16 @@ int kint_cache_attn_step(const kint_heads* q, const kint_heads* out, const kint_
     p.sorted = a.shape == SHAPE_CLUSTER && !window && B > 1 && B <= kMaxSorted && a.max_slabs >= 32 &&
                (long long)B * cache->kv_heads * a.tiles * a.blocks > a.slots;
     if (a.shape == SHAPE_CLUSTER) return traced("k_attn", s, [&] { return launch(ATTN_ONE); });
+    // (Asked first whether its blocks all run at once, as MinMax with many intervals leaves room for fewer than planned: a launch
+    // that the runtime refuses would end a stream's capture.)
     p.count = reinterpret_cast<int*>(ws + a.count);
-    const int units = B * cache->kv_heads * a.tiles;
-    if (cudaMemsetAsync(p.count, 0, (size_t)units * 2 * sizeof(int), s) != cudaSuccess) return KINT_ERR_LAUNCH;
-    cudaError_t e = cudaSuccess;
-    rc = traced("k_attn", s, [&] { return e = launch(ATTN_ONE); });
-    if (e != cudaErrorCooperativeLaunchTooLarge) return rc;
-    cudaGetLastError();  // (cleared: the two launches below do the work)
+    const cudaError_t fits = launch(ATTN_FITS);
+    if (fits == cudaSuccess) {
+      const int units = B * cache->kv_heads * a.tiles;
+      if (cudaMemsetAsync(p.count, 0, (size_t)units * 2 * sizeof(int), s) != cudaSuccess) return KINT_ERR_LAUNCH;
+      return traced("k_attn", s, [&] { return launch(ATTN_ONE); });
+    }
+    if (fits != cudaErrorCooperativeLaunchTooLarge) return KINT_ERR_LAUNCH;
   }
   p.nsplit = a.nsplit; p.per_split = a.per_split; p.big_words = 0;
   p.count = reinterpret_cast<int*>(ws + a.count);

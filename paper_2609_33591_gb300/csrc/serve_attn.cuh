@@ -44,6 +44,7 @@
 // keys (19 MB) 18 us; 8 requests of up to 1024 keys, 12 heads of 64, fp32 (4.3 MB) 9 us; one of 333 keys, 24 heads 5.8 us.
 #pragma once
 #include <atomic>
+#include <cstdint>
 #include <type_traits>
 
 #include "kint_dev.cuh"
@@ -1297,14 +1298,35 @@ cudaError_t want_smem(Kern kern, int bytes, int most, std::atomic<bool> (&grante
   return e;
 }
 
+// Whether `grid` blocks of `smem` dynamic bytes run at once on the current device.  The last answer is kept with its question, since
+// steps of one size ask the same again and again.
+template <class Kern>
+cudaError_t runs_at_once(Kern kern, int smem, int grid, std::atomic<uint64_t> (&known)[kMaxGranted]) {
+  int dev = 0, n = 0;
+  if (cudaError_t e = cudaGetDevice(&dev)) return e;
+  const bool keep = dev >= 0 && dev < kMaxGranted;
+  const uint64_t last = keep ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (last >> 32 == (uint32_t)smem) {
+    n = (int)(uint32_t)last;
+  } else {
+    if (cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, kThreads, (size_t)smem)) return e;
+    if (keep) known[dev].store((uint64_t)(uint32_t)smem << 32 | (uint32_t)n, std::memory_order_relaxed);
+  }
+  return (long long)n * serve_num_sms() >= grid ? cudaSuccess : cudaErrorCooperativeLaunchTooLarge;
+}
+
 template <int D, int NT, bool FOUR, bool F32, int MODE>
 cudaError_t go(const AttnP& p, int what, int grid, cudaStream_t s) {
   const int tab = MODE == M_GRID ? (p.calib == CAL_MINMAX ? 8 * NT : 1) * table_len(p.Kint) * (int)sizeof(float2) : 0;
   constexpr int kSums = kWarps * 8 * NT * D * (int)sizeof(float), kTab = MODE == M_GRID ? 8 * NT * table_len(KMAX) * (int)sizeof(float2) : 0;
-  if (what == ATTN_ONE) {
+  if (what == ATTN_ONE || what == ATTN_FITS) {
     const int smem = Ring<D>::kBytes + p.big_words * 4 + tab;
     static std::atomic<bool> granted[kMaxGranted];
     if (cudaError_t e = want_smem(k_attn<D, NT, FOUR, F32, MODE>, smem, Ring<D>::kBytes + kMaxScoreWords * 4 + kTab, granted)) return e;
+    if (what == ATTN_FITS) {
+      static std::atomic<uint64_t> known[kMaxGranted];
+      return runs_at_once(k_attn<D, NT, FOUR, F32, MODE>, smem, grid, known);
+    }
     if (p.count) return launch_cooperative(k_attn<D, NT, FOUR, F32, MODE>, dim3(grid), dim3(kThreads), smem, s, p);
     return launch_pdl_cluster(k_attn<D, NT, FOUR, F32, MODE>, dim3(grid), dim3(kThreads), smem, p.nsplit, s, p);
   }

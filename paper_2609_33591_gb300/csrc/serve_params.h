@@ -112,7 +112,8 @@ cudaError_t launch_rope_table(const RopeTableP& p, cudaStream_t s);
 cudaError_t launch_rope(const RopeP& p, int nsm, cudaStream_t s);
 cudaError_t launch_append(CacheIoP p, int nsm, cudaStream_t s);
 cudaError_t launch_read(CacheIoP p, int nsm, cudaStream_t s);
-enum AttnKernel : int { ATTN_ONE = 0, ATTN_SCORES = 1, ATTN_VALUES = 2 };
+// (ATTN_FITS launches nothing: whether ATTN_ONE's blocks, as a cooperative launch, run at once)
+enum AttnKernel : int { ATTN_ONE = 0, ATTN_SCORES = 1, ATTN_VALUES = 2, ATTN_FITS = 3 };
 cudaError_t launch_attn_64(const AttnP& p, int what, cudaStream_t s);
 cudaError_t launch_attn_128(const AttnP& p, int what, cudaStream_t s);
 
