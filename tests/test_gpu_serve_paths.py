@@ -56,6 +56,26 @@ def check(way, long, requests, heads, kv, new, d, calib, dtype, K=8, max_len=Non
 TILES = [(4, 1), (1, 4), (8, 1), (2, 3), (16, 1), (5, 4)]
 
 
+@pytest.mark.parametrize("calib,dtype", [(SOFT, F32), (SOFT, BF16), (FWM, BF16), (FWM, F32), (MM, F16), (RESOLVED, F32)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,new", TILES)
+def test_blocks_that_run_together(heads, new, d, calib, dtype):
+    check(TOGETHER, 9100, 3, heads, 1, new, d, calib, dtype)
+
+
+@pytest.mark.parametrize("calib,dtype", [(SOFT, F32), (SOFT, BF16), (FWM, BF16), (FWM, F32), (MM, F16), (RESOLVED, F32)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,new", TILES)
+def test_two_launches(heads, new, d, calib, dtype):
+    check(TWO, 8700 if heads * new > 8 else 16500, 39, heads, 1, new, d, calib, dtype)
+
+
+@pytest.mark.parametrize("heads,new", TILES)
+def test_clusters_with_the_larger_share_of_shared_memory(heads, new):
+    """As long as clusters go: 32 KB of scores a block (tiles of four rows), 48 and 56 KB."""
+    check(CLUSTER, 16000 if heads * new <= 4 else 12000 if heads * new <= 8 else 7000, 40, heads, 1, new, 64, MM, F32, K=64)
+
+
 @pytest.mark.parametrize("heads,new", [(4, 1), (1, 3)])
 def test_blocks_that_do_not_fit_at_once(heads, new):
     """MinMax with many intervals: its tables leave room for fewer blocks than the launch was planned with."""
