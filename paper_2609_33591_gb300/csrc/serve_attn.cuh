@@ -801,11 +801,12 @@ __device__ __forceinline__ void value_pass(const AttnP& p, const Share& sh, cons
         float2 x0 = mul2(w[n][0], s0), x1 = mul2(w[n][1], s1);
         if (all) {
           cs[n][k] = fma2(w[n][0], c0, fma2(w[n][1], c1, cs[n][k]));
-        } else {  // a key that is not seen adds nothing, whatever its place holds
-          if (w[n][0].x == 0.0f) x0.x = 0.0f; else cs[n][k].x = fmaf(w[n][0].x, c0.x, cs[n][k].x);
-          if (w[n][0].y == 0.0f) x0.y = 0.0f; else cs[n][k].y = fmaf(w[n][0].y, c0.y, cs[n][k].y);
-          if (w[n][1].x == 0.0f) x1.x = 0.0f; else cs[n][k].x = fmaf(w[n][1].x, c1.x, cs[n][k].x);
-          if (w[n][1].y == 0.0f) x1.y = 0.0f; else cs[n][k].y = fmaf(w[n][1].y, c1.y, cs[n][k].y);
+        } else {  // a key that is not seen adds nothing, whatever its place holds; one that is seen does, a NaN with no weight too
+          const float2 v0 = *reinterpret_cast<const float2*>(sc + n * 128 + k0), v1 = *reinterpret_cast<const float2*>(sc + n * 128 + k1);
+          if (v0.x == kMasked) x0.x = 0.0f; else cs[n][k].x = fmaf(w[n][0].x, c0.x, cs[n][k].x);
+          if (v0.y == kMasked) x0.y = 0.0f; else cs[n][k].y = fmaf(w[n][0].y, c0.y, cs[n][k].y);
+          if (v1.x == kMasked) x1.x = 0.0f; else cs[n][k].x = fmaf(w[n][1].x, c1.x, cs[n][k].x);
+          if (v1.y == kMasked) x1.y = 0.0f; else cs[n][k].y = fmaf(w[n][1].y, c1.y, cs[n][k].y);
         }
         if constexpr (FOUR) {
           b0[n][0] = part_f16(x0, take);

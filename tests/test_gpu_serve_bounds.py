@@ -1,5 +1,6 @@
 """GPU: what the serving operators do at and past the bounds that a caller states, and with rows, blocks and memory that
 belong to nobody.  Tolerances are those of test_gpu_serve.py; the rest is equality."""
+import math
 import threading
 
 import numpy as np
@@ -201,3 +202,22 @@ def test_a_step_that_refuses_a_request():
     with pytest.raises(ValueError):
         serve.attention(torch.zeros(2, 4, 64, device="cuda"), cache.pages[0], cache.table, plan.lens, plan.cu, kint.Config(),
                         slots=plan.slots[:1])
+
+
+@pytest.mark.parametrize("calib,recon", [(FWM, LERP), (FWM, kint.RECON_NEAREST), (kint.CALIB_EXP_FP8, LERP), (SOFT, LERP)])
+@pytest.mark.parametrize("place", [3, 36])
+def test_a_value_that_is_seen_with_no_weight_still_shows_its_nan(calib, recon, place):
+    """0 times NaN is NaN whether the key's slab is seen in full or lies at the end of the list (40 keys: slabs 0 and 2), and
+    only in the 64 channels that hold it; a key that is not seen stays out."""
+    k, v = torch.randn(40, 1, 128), torch.randn(40, 1, 128)
+    k[:, :, 0], q = 1.0, torch.zeros(1, 2, 128)
+    q[..., 0] = 3000.0
+    k[place, 0, 0] = -1.0   # a score some 500 below the others': weight 0 (under softmax below the smallest number)
+    v[place, 0, 70] = math.nan
+    pages, table = serve.cache_pages(2, 64, 1, 128), ints([[1]])
+    serve.append(gpu(k), gpu(v), 64 + torch.arange(40, device="cuda"), pages)
+    cfg = kint.Config(Kint=4, calib=calib, tau=3.0, recon=recon)
+    for n, shows in ((40, True), (place, False)):
+        o = serve.attention(gpu(q), pages, table, ints([n]), ints([0, 1]), cfg)
+        assert torch.isfinite(o[..., :64]).all()
+        assert torch.isnan(o[..., 64:]).all() if shows else torch.isfinite(o[..., 64:]).all()
