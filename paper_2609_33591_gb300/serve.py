@@ -165,20 +165,21 @@ def rope(q, k, pos, table, *, interleaved: bool = False, inverse: bool = False, 
 
 
 class RotaryFn(torch.autograd.Function):
-    """rope as a differentiable op: the gradients are turned back by the inverse rotation."""
+    """rope as a differentiable op: gradients are turned back by the inverse rotation, which is this op again, so derivatives of
+    every order follow."""
 
     @staticmethod
-    def forward(ctx, q, k, pos, table, interleaved: bool):
+    def forward(ctx, q, k, pos, table, interleaved: bool, inverse: bool = False):
         ctx.save_for_backward(pos, table)
-        ctx.interleaved = interleaved
-        return rope(q, k, pos, table, interleaved=interleaved)
+        ctx.interleaved, ctx.inverse = interleaved, inverse
+        return rope(q, k, pos, table, interleaved=interleaved, inverse=inverse)
 
     @staticmethod
     def backward(ctx, dq, dk):
         pos, table = ctx.saved_tensors
         dq, dk = (x if x.stride(-1) == 1 else x.contiguous() for x in (dq, dk))
-        dq, dk = rope(dq, dk, pos, table, interleaved=ctx.interleaved, inverse=True)
-        return dq, dk, None, None, None
+        dq, dk = RotaryFn.apply(dq, dk, pos, table, ctx.interleaved, not ctx.inverse)
+        return dq, dk, None, None, None, None
 
 
 def rotary(q, k, pos, table, interleaved: bool = False):

@@ -1,0 +1,61 @@
+"""GPU: the serving operators next to autograd: derivatives of the rotation of every order and type, and what is not
+differentiable, or writes into its arguments, says so."""
+import pytest
+import torch
+
+from paper_2609_33591_gb300 import kint, serve
+from tests import serve_ref as ref
+from tests.test_gpu_serve import BF16, F16, F32, HALF_UNIT, SOFT, _clean, _lib, filled, gpu, ints  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def plain(x, pos, table, interleaved):
+    """The rotation in elementary torch operations, x and table in 64 bits, differentiable."""
+    half = table.size(1)
+    cs = table[pos.long()][:, :, None]
+    i = torch.arange(half, device=x.device)
+    ia, ib = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+    a, b = x[..., ia], x[..., ib]
+    y = torch.empty_like(x)
+    y[..., 2 * half:] = x[..., 2 * half:]
+    y[..., ia], y[..., ib] = a * cs[..., 0] - b * cs[..., 1], b * cs[..., 0] + a * cs[..., 1]
+    return y
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_second_derivatives_of_the_rotation(interleaved):
+    """L = sum c * dL1/dq with L1 = sum(a^3) + sum(a b): what goes through the rotation twice counts.  All fp32; each number is
+    a sum of a few products of at most three rotated channels, so 2^-18 of the largest."""
+    table = serve.rope_table(40, 48)
+    pos = torch.randint(0, 40, (2, 6), device="cuda").int()
+    q, k, c = (torch.randn(2, 6, 3, 64, device="cuda") for _ in range(3))
+
+    def second(q, k, c, turn):
+        q, k = q.clone().requires_grad_(), k.clone().requires_grad_()
+        a, b = turn(q, k)
+        g, = torch.autograd.grad((a ** 3).sum() + (a * b).sum(), q, create_graph=True)
+        return torch.autograd.grad((g * c).sum(), (q, k))
+
+    got = second(q, k, c, lambda q, k: serve.rotary(q, k, pos, table, interleaved))
+    want = second(q.double(), k.double(), c.double(), lambda q, k: tuple(plain(x, pos, table.double(), interleaved) for x in (q, k)))
+    for x, y in zip(got, want):
+        assert (x.double() - y).abs().max() <= 2.0 ** -18 * y.abs().max()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_gradients_of_every_type(dtype, interleaved):
+    table = serve.rope_table(40, 64)
+    pos = torch.randint(0, 40, (1, 9), device="cuda").int()
+    q, k = (torch.randn(1, 9, h, 64, device="cuda").to(dtype).requires_grad_() for h in (4, 2))
+    c = [torch.randn_like(x) for x in (q, k)]
+    grads = torch.autograd.grad(serve.rotary(q, k, pos, table, interleaved), (q, k), c)
+    for g, x in zip(grads, c):
+        want = ref.rotate(x.cpu(), pos.cpu(), table.cpu(), 64, interleaved, inverse=True)
+        size = 2 * x.detach().cpu().double().abs().amax(-1, keepdim=True)
+        assert g.dtype == dtype and ((g.cpu().double() - want).abs() <= HALF_UNIT[dtype] * want.abs() + 3 * 2.0 ** -24 * size).all()
+    # a gradient that one number is spread from (no strides of its own)
+    g, = torch.autograd.grad(serve.rotary(q, k, pos, table, interleaved)[0].sum(), q)
+    want = ref.rotate(torch.ones(1, 9, 4, 64), pos.cpu(), table.cpu(), 64, interleaved, inverse=True)
+    assert ((g.cpu().double() - want).abs() <= HALF_UNIT[dtype] * want.abs() + 6 * 2.0 ** -24).all()
