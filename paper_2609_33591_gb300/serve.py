@@ -177,13 +177,13 @@ class RotaryFn(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dq, dk):
         pos, table = ctx.saved_tensors
-        dq, dk = (x if x.stride(-1) == 1 else x.contiguous() for x in (dq, dk))
+        dq, dk = (x if x is None or x.stride(-1) == 1 else x.contiguous() for x in (dq, dk))
         dq, dk = RotaryFn.apply(dq, dk, pos, table, ctx.interleaved, not ctx.inverse)
         return dq, dk, None, None, None, None
 
 
 def rotary(q, k, pos, table, interleaved: bool = False):
-    """Differentiable rotary positions of q and k [B, T, heads, d]."""
+    """Differentiable rotary positions of q and k (or None) [B, T, heads, d]."""
     return RotaryFn.apply(q, k, pos, table, interleaved)
 
 

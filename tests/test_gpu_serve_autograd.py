@@ -59,3 +59,16 @@ def test_gradients_of_every_type(dtype, interleaved):
     g, = torch.autograd.grad(serve.rotary(q, k, pos, table, interleaved)[0].sum(), q)
     want = ref.rotate(torch.ones(1, 9, 4, 64), pos.cpu(), table.cpu(), 64, interleaved, inverse=True)
     assert ((g.cpu().double() - want).abs() <= HALF_UNIT[dtype] * want.abs() + 6 * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_queries_alone(interleaved):
+    """rotary without keys, forward and back."""
+    table = serve.rope_table(40, 64)
+    pos = torch.randint(0, 40, (7,), device="cuda").int()
+    q = torch.randn(2, 7, 3, 64, device="cuda", requires_grad=True)
+    c = torch.randn(2, 7, 3, 64, device="cuda")
+    a, none = serve.rotary(q, None, pos, table, interleaved)
+    assert none is None and torch.equal(a, serve.rope(q.detach(), None, pos, table, interleaved=interleaved)[0])
+    a.backward(c)
+    assert torch.equal(q.grad, serve.rope(c, None, pos, table, interleaved=interleaved, inverse=True)[0])
