@@ -276,6 +276,8 @@ class KIntServingAttention(KIntSelfAttention):
         H, D = self.n_head, C // self.n_head
         if self.window and self.window < T:
             raise ValueError("the training forward is full causal attention: T may not exceed the window")
+        if pos is None:
+            _need(T <= self.rope.size(0), f"T = {T} is past the layer's max_pos, {self.rope.size(0)}")
         q, k, v = (t.view(B, T, H, D) for t in self.c_attn(x).split(C, dim=2))
         pos = torch.arange(T, dtype=torch.int32, device=x.device) if pos is None else pos
         q, k = rotary(q, k, pos, self.rope, self.interleaved)
@@ -290,9 +292,11 @@ class KIntServingAttention(KIntSelfAttention):
         the plan refused get the projection of zeros."""
         rows, C = x.shape
         D = C // self.n_head
+        max_len = max_len or cache.max_len
+        _need(max_len <= self.rope.size(0), f"requests of up to {max_len} tokens are past the layer's max_pos, {self.rope.size(0)}")
         q, k, v = (t.view(rows, self.n_head, D) for t in self.c_attn(x).split(C, dim=1))
         pages = cache.pages[layer]
         q = append(k, v, plan.slots, pages, q=q, pos=plan.pos, table=self.rope, interleaved=self.interleaved)
         y = attention(q, pages, cache.table, plan.lens, plan.cu, self.cfg, window=self.window, sinks=self.sinks,
-                      max_new=max_new, max_len=max_len or cache.max_len, slots=plan.slots)
+                      max_new=max_new, max_len=max_len, slots=plan.slots)
         return self.c_proj(y.view(rows, C))

@@ -1,0 +1,25 @@
+"""GPU: the serving layer, the cache that it keeps, and the smaller calls at their edges."""
+import pytest
+import torch
+
+from paper_2609_33591_gb300 import kint, serve
+from tests.test_gpu_serve import BF16, F16, F32, FWM, _clean, _lib, expect_flag, ints  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def test_positions_that_the_table_does_not_hold_are_refused():
+    """Sequences and caches longer than the layer's rotations: an error, not rows without a rotation."""
+    layer = serve.KIntServingAttention(256, 4, kint.Config(), max_pos=32)
+    assert layer(torch.randn(1, 32, 256, device="cuda")).shape == (1, 32, 256)
+    with pytest.raises(ValueError, match="max_pos"):
+        layer(torch.randn(1, 33, 256, device="cuda"))
+    cache = serve.PagedCache(1, 1, 64, 8, 4, 64, block_size=16)
+    x = torch.randn(4, 256, device="cuda")
+    plan = cache.extend(ints([4]), 4)
+    with pytest.raises(ValueError, match="max_pos"):
+        layer.step(x, cache, plan)
+    with pytest.raises(ValueError, match="max_pos"):
+        layer.step(x, cache, plan, max_len=33)
+    assert not cache.pages.any()
+    assert layer.step(x, cache, plan, max_len=32).shape == x.shape  # a shorter bound than the cache's
