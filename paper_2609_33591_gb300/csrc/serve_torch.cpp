@@ -277,6 +277,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     kint_heads hq{}, hqo{};
     at::Tensor qo;
     const bool has_q = !none(a[4]), turn = has_q && tab.ptr;
+    need(turn || none(a[8]), "q_out: expected with q and a rotation only");
     if (has_q) {
       const at::Tensor& q = tensor(a[4], "q");
       need(q.dim() == 3 && q.size(0) == tokens && q.size(2) == c.d && q.scalar_type() == k.scalar_type(), "q and k disagree");

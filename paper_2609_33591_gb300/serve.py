@@ -198,7 +198,8 @@ def cache_pages(num_blocks: int, block_size: int, kv_heads: int, d: int, *, devi
 
 def append(k, v, slots, pages, *, q=None, pos=None, table=None, interleaved: bool = False, q_out=None, stream=None):
     """New tokens' k and v [tokens, kv_heads, d] into the cache at slots [tokens] (int64; -1: skipped), the keys rotated
-    to pos [tokens] where a table is given.  Returns q [tokens, heads, d] rotated likewise (None without q)."""
+    to pos [tokens] where a table is given.  Returns q [tokens, heads, d] rotated likewise, in q_out if given (without a table
+    q itself, without q None)."""
     return (_mod or _ext()).append(k, v, slots, pages, q, pos, table, interleaved, q_out, _handle(stream))
 
 

@@ -23,3 +23,13 @@ def test_positions_that_the_table_does_not_hold_are_refused():
         layer.step(x, cache, plan, max_len=33)
     assert not cache.pages.any()
     assert layer.step(x, cache, plan, max_len=32).shape == x.shape  # a shorter bound than the cache's
+
+
+def test_a_buffer_for_queries_that_are_not_rotated_is_refused():
+    x, buf = torch.randn(3, 2, 64, device="cuda"), torch.full((3, 2, 64), 7.0, device="cuda")
+    pages, slots = serve.cache_pages(1, 16, 2, 64), ints([0, 1, 2], torch.int64)
+    for kw in (dict(q=x), dict(), dict(table=serve.rope_table(4, 64), pos=ints([0, 1, 2]))):
+        with pytest.raises(ValueError, match="q_out"):
+            serve.append(x, x, slots, pages, q_out=buf, **kw)
+    assert not pages.any() and (buf == 7.0).all()
+    assert serve.append(x, x, slots, pages, q=x) is x and serve.append(x, x, slots, pages) is None
