@@ -240,7 +240,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     need(qo.sizes() == q.sizes() && qo.scalar_type() == q.scalar_type() &&
              (!k || (ko.sizes() == k->sizes() && ko.scalar_type() == k->scalar_type())),
          "out disagrees with q and k");
-    if (q.numel()) {
+    if (q.numel() || (k && k->numel())) {
       const kint_heads ho = heads(qo, "out", 4), hko = k ? heads(ko, "out", 4) : kint_heads{};
       run(api.rope(&hq, &ho, &hk, &hko, pp, pos.dim() == 2 ? pos.stride(0) : 0, tab.ptr, tab.max_pos, (int)B, (int)T, (int)q.size(3),
                    tab.rot, PyObject_IsTrue(a[4]), PyObject_IsTrue(a[5]), type_of(q, "q"), stream.handle),

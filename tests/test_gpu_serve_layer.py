@@ -33,3 +33,15 @@ def test_a_buffer_for_queries_that_are_not_rotated_is_refused():
             serve.append(x, x, slots, pages, q_out=buf, **kw)
     assert not pages.any() and (buf == 7.0).all()
     assert serve.append(x, x, slots, pages, q=x) is x and serve.append(x, x, slots, pages) is None
+
+
+@pytest.mark.parametrize("hq,hk", [(0, 2), (2, 0)])
+@pytest.mark.parametrize("place", [False, True])
+def test_rope_of_one_of_two(hq, hk, place):
+    """Queries or keys of no heads: the other is rotated."""
+    table, pos = serve.rope_table(8, 64), ints([0, 1, 5])
+    q, k = torch.randn(2, 3, hq, 64, device="cuda"), torch.randn(2, 3, hk, 64, device="cuda")
+    x = q if hq else k
+    want = serve.rope(x, None, pos, table)[0]
+    a, b = serve.rope(q, k, pos, table, out=(q, k) if place else None)
+    assert torch.equal(a if hq else b, want) and a.shape == q.shape and b.shape == k.shape
