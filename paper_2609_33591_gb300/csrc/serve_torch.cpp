@@ -141,6 +141,10 @@ at::Tensor part(const at::Tensor& base, at::ScalarType type, int64_t at, at::Int
   return t;
 }
 int64_t up_to(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
+// A tensor of the caller's that the call wrote into counts one change more, so that autograd notices where it was saved before.
+void wrote(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // An output like `x`: its strides where they fill its memory, else contiguous.
 at::IntArrayRef like(const at::Tensor& x) { return x.is_non_overlapping_and_dense() ? x.strides() : at::IntArrayRef(); }
 
@@ -207,6 +211,7 @@ PyObject* extend_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
                           o + at_lens, o + at_free, o + at_cu, reinterpret_cast<int64_t*>(o), o + at_pos, o + at_req, o + at_ref,
                           stream.handle),
         "kint_blocks_extend");
+    wrote(table);
     auto ints_at = [&](int64_t at, int64_t n) { return wrap(part(out, at::kInt, at, {n}, {})); };
     return Py_BuildValue("(NNNNNNN)", ints_at(at_lens, B), ints_at(at_cu, B + 1), wrap(part(out, at::kLong, 0, {tokens}, {})),
                          ints_at(at_pos, tokens), ints_at(at_req, tokens), ints_at(at_free, 1), ints_at(at_ref, 1));
@@ -245,6 +250,10 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
       run(api.rope(&hq, &ho, &hk, &hko, pp, pos.dim() == 2 ? pos.stride(0) : 0, tab.ptr, tab.max_pos, (int)B, (int)T, (int)q.size(3),
                    tab.rot, PyObject_IsTrue(a[4]), PyObject_IsTrue(a[5]), type_of(q, "q"), stream.handle),
           "kint_rope");
+      if (!none(a[6])) {
+        wrote(qo);
+        if (k) wrote(ko);
+      }
     }
     PyObject* second = Py_None;
     if (k)
@@ -288,10 +297,13 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         hqo = heads(qo, "q_out", 3);
       }
     }
-    if (tokens)
+    if (tokens) {
       run(api.append(&c, &hk, &hv, ints<int64_t>(slots, "slots"), (int)tokens, turn ? &hq : nullptr, turn ? &hqo : nullptr, pos, tab.ptr,
                      tab.max_pos, tab.rot, PyObject_IsTrue(a[7]), type_of(k, "k"), stream.handle),
           "kint_cache_append");
+      wrote(pages);
+      if (!none(a[8])) wrote(qo);
+    }
     if (turn) return wrap(qo);
     Py_INCREF(a[4]);
     return a[4];  // q as it came, or None
@@ -365,6 +377,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
                    (float)tau, (kint_recon)whole(a[8]), max_new, max_len, type_of(q, "q"), slots, none(a[13]), ws.data_ptr(), ws.is_same(pages) ? kUnusedWorkspace : ws.nbytes(),
                    stream.handle),
           "kint_cache_attn");
+      if (!none(a[13])) wrote(out);
     }
     return wrap(out);
   });

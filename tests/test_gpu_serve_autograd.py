@@ -72,3 +72,34 @@ def test_queries_alone(interleaved):
     assert none is None and torch.equal(a, serve.rope(q.detach(), None, pos, table, interleaved=interleaved)[0])
     a.backward(c)
     assert torch.equal(q.grad, serve.rope(c, None, pos, table, interleaved=interleaved, inverse=True)[0])
+
+
+def test_writing_into_an_argument_counts_as_a_change_of_it():
+    """Autograd notices that a tensor it saved was overwritten."""
+    table, pos = serve.rope_table(8, 64), ints([0, 1, 2])
+    pages, slots = serve.cache_pages(2, 16, 2, 64), ints([0, 1, 2], torch.int64)
+    x = torch.randn(3, 2, 64, device="cuda")
+    q, k, o = x.clone()[None], x.clone()[None], torch.empty_like(x)
+    blocks, free = torch.full((1, 2), -1, dtype=torch.int32, device="cuda"), ints([0, 1])
+
+    def changed(t, call):
+        before = t._version
+        call()
+        return t._version > before
+
+    assert changed(q, lambda: serve.rope(q, k, pos, table, out=(q, k)))
+    assert changed(k, lambda: serve.rope(q, k, pos, table, out=(q, k)))
+    assert changed(pages, lambda: serve.append(x, x, slots, pages))
+    assert changed(o, lambda: serve.append(x, x, slots, pages, q=x, q_out=o, pos=pos, table=table))
+    assert changed(o, lambda: serve.attention(x, pages, ints([[0, 1]]), ints([3]), ints([0, 3]), kint.Config(calib=SOFT), out=o))
+    assert changed(blocks, lambda: serve.extend_blocks(ints([0]), ints([3]), blocks, free, ints([2]), 16, 3))
+    assert not changed(x, lambda: serve.rope(x[None], None, pos, table))
+    w = torch.randn_like(q).requires_grad_()
+    y = w * q
+    serve.rope(q, k, pos, table, out=(q, k))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    with torch.inference_mode():
+        t = x.clone()
+        assert torch.equal(serve.rope(t[None], None, pos, table, out=(t[None], None))[0][0],
+                           serve.rope(x[None], None, pos, table)[0][0])
