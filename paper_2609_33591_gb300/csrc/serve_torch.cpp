@@ -4,11 +4,14 @@
 //
 // The library's functions are handed over as addresses (bind), so this module links against
 // torch and Python only.
+#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -145,6 +148,16 @@ int64_t up_to(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 void wrote(const at::Tensor& t) {
   if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
+// Calls whose result has no derivative here: where one is asked for, the result says so when it is needed, instead of passing for a
+// constant, and a buffer for it is refused.
+bool asked(const at::Tensor& x) { return x.requires_grad() && c10::GradMode::is_enabled(); }
+void plain_buffer(const at::Tensor& x, const at::Tensor& out) {
+  need(!asked(x) && !asked(out), "a buffer for the result is not taken where gradients are asked for");
+}
+void no_derivative(at::Tensor& y, const at::Tensor& x, const char* what) {
+  if (asked(x))
+    torch::autograd::set_history(y, std::make_shared<torch::autograd::NotImplemented>(what, torch::autograd::collect_next_edges(x)));
+}
 // An output like `x`: its strides where they fill its memory, else contiguous.
 at::IntArrayRef like(const at::Tensor& x) { return x.is_non_overlapping_and_dense() ? x.strides() : at::IntArrayRef(); }
 
@@ -240,7 +253,11 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (k) ko = part(both, q.scalar_type(), nq, k->sizes(), like(*k));
     } else {
       qo = tensor(a[6], "out");
-      if (k) ko = tensor(a[7], "out");
+      plain_buffer(q, qo);
+      if (k) {
+        ko = tensor(a[7], "out");
+        plain_buffer(*k, ko);
+      }
     }
     need(qo.sizes() == q.sizes() && qo.scalar_type() == q.scalar_type() &&
              (!k || (ko.sizes() == k->sizes() && ko.scalar_type() == k->scalar_type())),
@@ -255,6 +272,8 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (k) wrote(ko);
       }
     }
+    no_derivative(qo, q, "rope (rotary is)");
+    if (k) no_derivative(ko, *k, "rope (rotary is)");
     PyObject* second = Py_None;
     if (k)
       second = wrap(ko);
@@ -292,6 +311,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       need(q.dim() == 3 && q.size(0) == tokens && q.size(2) == c.d && q.scalar_type() == k.scalar_type(), "q and k disagree");
       if (turn) {
         qo = none(a[8]) ? at::empty_like(q) : tensor(a[8], "q_out");
+        if (!none(a[8])) plain_buffer(q, qo);
         need(qo.sizes() == q.sizes() && qo.scalar_type() == q.scalar_type(), "q_out disagrees with q");
         hq = heads(q, "q", 3);
         hqo = heads(qo, "q_out", 3);
@@ -304,7 +324,10 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       wrote(pages);
       if (!none(a[8])) wrote(qo);
     }
-    if (turn) return wrap(qo);
+    if (turn) {
+      no_derivative(qo, tensor(a[4], "q"), "append");
+      return wrap(qo);
+    }
     Py_INCREF(a[4]);
     return a[4];  // q as it came, or None
   });
@@ -359,6 +382,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const CallStream stream(a[16]);
     at::Tensor out = none(a[13]) ? at::empty_like(q) : tensor(a[13], "out");
     need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out disagrees with q");
+    if (!none(a[13])) plain_buffer(q, out);
     if (q.numel()) {
       const kint_heads ho = heads(out, "out", 3);
       at::Tensor ws;
@@ -379,6 +403,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
           "kint_cache_attn");
       if (!none(a[13])) wrote(out);
     }
+    no_derivative(out, q, "attention over the cache");
     return wrap(out);
   });
 }

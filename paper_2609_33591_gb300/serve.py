@@ -8,6 +8,9 @@ given, to which the memory that a call allocates then belongs.  One step of a la
     q = append(k, v, plan.slots, pages, q=q, pos=plan.pos, table=rope)
     o = attention(q, pages, blocks, plan.lens, plan.cu, cfg, slots=plan.slots, ...)
 
+Only ``rotary`` is differentiable.  The other calls' results raise where a gradient through them is asked for (keys and values
+end in the cache, whose codes have none).
+
 ``PagedCache`` keeps the tables and lengths between steps, ``rotary`` is the differentiable
 rotation for training, and ``KIntServingAttention`` is the GPT-2 block of ``attention`` with
 rotary positions, a training forward and a serving step.

@@ -103,3 +103,32 @@ def test_writing_into_an_argument_counts_as_a_change_of_it():
         t = x.clone()
         assert torch.equal(serve.rope(t[None], None, pos, table, out=(t[None], None))[0][0],
                            serve.rope(x[None], None, pos, table)[0][0])
+
+
+def test_what_is_not_differentiable_says_so():
+    """Results of inputs that require gradients are the same numbers; asking for the gradient raises.  Without gradients asked
+    for, nothing is recorded."""
+    table, pos = serve.rope_table(8, 64), ints([0, 1, 2])
+    pool = filled([16], 2, 64, 32, 3)
+    pages, slots = gpu(pool.pages), ints([13, 14, 15], torch.int64)
+    x = torch.randn(3, 2, 64, device="cuda")
+    attend = lambda q, **kw: serve.attention(q, pages, gpu(pool.table), gpu(pool.lens), ints([0, 3]), kint.Config(), **kw)  # noqa: E731
+    turn = lambda q, **kw: serve.rope(q[None], None, pos, table, **kw)[0]  # noqa: E731
+    turn_k = lambda k: serve.rope(x[None], k[None], pos, table)[1]  # noqa: E731
+    append = lambda q, **kw: serve.append(x, x, slots, pages, q=q, pos=pos, table=table, **kw)  # noqa: E731
+    for call in (attend, turn, turn_k, append):
+        leaf = x.clone().requires_grad_()
+        y = call(leaf)
+        assert torch.equal(y.detach(), call(x)) and y.requires_grad and not call(x).requires_grad
+        with pytest.raises(RuntimeError, match="not implemented"):
+            y.sum().backward()
+        with torch.no_grad():
+            assert not call(leaf).requires_grad
+    for call, out in ((attend, torch.empty_like(x)), (append, None), (turn, (torch.empty_like(x)[None], None))):
+        kw = dict(q_out=torch.empty_like(x)) if out is None else dict(out=out)
+        with pytest.raises(ValueError):
+            call(x.clone().requires_grad_(), **kw)
+    w = x.clone().requires_grad_()
+    with pytest.raises(ValueError):  # into what gradients are asked of
+        attend(x, out=w)
+    assert torch.equal(w.detach(), x)
