@@ -275,6 +275,13 @@ class KIntServingAttention(KIntSelfAttention):
         self.register_buffer("rope", rope_table(max_pos, rot or n_embd // n_head, base, device=device, **scaling),
                              persistent=False)
 
+    def _apply(self, fn, recurse=True):
+        rope = self.rope if "rope" in self._buffers else None
+        super()._apply(fn, recurse)
+        if rope is not None and self.rope.dtype != rope.dtype:  # a cast of the layer is not one of its angles' cosines and sines
+            self.rope = rope.to(self.rope.device)
+        return self
+
     def forward(self, x, pos=None):
         B, T, C = x.shape
         H, D = self.n_head, C // self.n_head
