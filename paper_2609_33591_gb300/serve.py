@@ -152,9 +152,10 @@ def rope_frequencies(rot: int, base: float = 10000.0, *, scaling: str | None = N
 def rope_table(max_pos: int, rot: int, base: float = 10000.0, *, device="cuda", stream=None, **scaling) -> torch.Tensor:
     """(cos, sin) pairs [max_pos, rot / 2, 2], fp32 (angles and functions in fp64); keywords as rope_frequencies."""
     freq, mag = rope_frequencies(rot, base, **scaling)
-    table = torch.empty(max_pos, rot // 2, 2, dtype=torch.float32, device=device)
-    handle = torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
-    rc = load().kint_rope_table(table.data_ptr(), max_pos, rot, (ctypes.c_double * len(freq))(*freq), mag, handle)
+    with torch.cuda.stream(stream):  # (None: the current one)
+        table = torch.empty(max_pos, rot // 2, 2, dtype=torch.float32, device=device)
+        handle = torch.cuda.current_stream().cuda_stream
+        rc = load().kint_rope_table(table.data_ptr(), max_pos, rot, (ctypes.c_double * len(freq))(*freq), mag, handle)
     if rc:
         raise kint.KintError(rc, "kint_rope_table")
     return table

@@ -65,3 +65,26 @@ def test_the_layer_in_another_type(dtype):
         cache = serve.PagedCache(1, 1, 64, 4, 4, 64, block_size=16)
         s = layer.step(x[0].to(dtype), cache, cache.extend(ints([20]), 20), max_new=20)
         assert s.dtype == dtype and (s.float() - want[0]).norm() <= 0.3 * want.norm()
+
+
+def owner(t):
+    """The stream that t's memory belongs to."""
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= t.data_ptr() < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+
+
+def test_memory_belongs_to_the_stream_that_is_given():
+    """On another stream than the current one nothing orders the current stream's use of a block of memory and the call's."""
+    side = torch.cuda.Stream()
+    table = serve.rope_table(16, 64, stream=side)
+    pages = serve.cache_pages(2, 16, 2, 64)
+    x, slots, pos = torch.randn(3, 2, 64, device="cuda"), ints([0, 1, 2], torch.int64), ints([0, 1, 2])
+    torch.cuda.synchronize()
+    made = [table, serve.rope(x[None], None, pos, table, stream=side)[0], serve.read(pages, slots, stream=side)[0],
+            serve.append(x, x, slots, pages, q=x, pos=pos, table=table, stream=side),
+            serve.attention(x, pages, ints([[0, 1]]), ints([3]), ints([0, 3]), kint.Config(), stream=side),
+            serve.extend_blocks(ints([0]), ints([3]), ints([[-1]]), ints([0]), ints([1]), 16, 3, stream=side).slots]
+    side.synchronize()
+    assert [owner(t) for t in made] == [side.cuda_stream] * len(made)
+    assert torch.equal(table, serve.rope_table(16, 64))
