@@ -239,7 +239,7 @@ class PagedCache:
     def __init__(self, layers: int, requests: int, max_len: int, num_blocks: int, kv_heads: int, d: int, *,
                  block_size: int = 32, device="cuda"):
         self.block_size, self.max_len = block_size, max_len
-        self.pages = torch.stack([cache_pages(num_blocks, block_size, kv_heads, d, device=device) for _ in range(layers)])
+        self.pages = cache_pages(layers * num_blocks, block_size, kv_heads, d, device=device).unflatten(0, (layers, num_blocks))
         width = -(-max_len // block_size)
         i32 = dict(dtype=torch.int32, device=device)
         self.table = torch.full((requests, width), -1, **i32)

@@ -88,3 +88,18 @@ def test_memory_belongs_to_the_stream_that_is_given():
     side.synchronize()
     assert [owner(t) for t in made] == [side.cuda_stream] * len(made)
     assert torch.equal(table, serve.rope_table(16, 64))
+
+
+def test_a_cache_takes_its_own_size_of_memory():
+    """Not its layers' pools twice over."""
+    torch.cuda.empty_cache()
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    cache = serve.PagedCache(8, 4, 4096, 2048, 8, 128, block_size=32)
+    assert torch.cuda.max_memory_allocated() - before <= 1.1 * cache.pages.numel()
+    assert cache.pages.shape == (8, 2048, 8, 2, 18 * 128) and not cache.pages.any()
+    for bad in (dict(block_size=24), dict(block_size=8)):
+        with pytest.raises(kint.KintError):
+            serve.PagedCache(1, 1, 64, 4, 4, 64, **bad)
+    with pytest.raises(kint.KintError):
+        serve.PagedCache(1, 1, 64, 4, 4, 96)
