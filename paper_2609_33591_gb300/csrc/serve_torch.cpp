@@ -210,6 +210,7 @@ PyObject* extend_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int block = whole(a[5]), tokens = whole(a[6]);
     need(lens.dim() == 1 && add.sizes() == lens.sizes() && table.dim() == 2 && table.size(0) == lens.size(0) && n_free.numel() == 1,
          "lens, new, table and n_free disagree on the requests");
+    need(list.dim() == 1, "free: expected one dimension");
     need(tokens >= 0, "tokens must not be negative");
     const int32_t *pl = ints<int32_t>(lens, "lens"), *pa = ints<int32_t>(add, "new"), *pf = ints<int32_t>(list, "free"),
                   *pn = ints<int32_t>(n_free, "n_free");

@@ -221,3 +221,12 @@ def test_a_value_that_is_seen_with_no_weight_still_shows_its_nan(calib, recon, p
         o = serve.attention(gpu(q), pages, table, ints([n]), ints([0, 1]), cfg)
         assert torch.isfinite(o[..., :64]).all()
         assert torch.isnan(o[..., 64:]).all() if shows else torch.isfinite(o[..., 64:]).all()
+
+
+def test_a_free_list_of_rows_is_refused():
+    """Only its last dimension's stride is looked at, so rows further apart (or on top of each other) would be read as one list."""
+    lens, new, table, n_free = ints([0]), ints([3]), ints([[-1]]), ints([4])
+    for free in (ints([[4, 5], [6, 7]]), ints([[4, 5, 0], [6, 7, 0]])[:, :2], ints([1]).expand(4, 1)):
+        with pytest.raises(ValueError, match="free"):
+            serve.extend_blocks(lens, new, table, free, n_free, 16, 3)
+    assert table.tolist() == [[-1]]
