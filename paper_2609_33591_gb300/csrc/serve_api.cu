@@ -23,9 +23,14 @@ int traced(const char* name, cudaStream_t s, F&& launch) {
 int elem_size(int dtype) { return dtype == KINT_FP32 ? 4 : 2; }
 bool valid_dtype(int t) { return t >= KINT_FP32 && t <= KINT_FP16; }
 
+constexpr int kMaxHeads = 1 << 24;
+// Tokens of an append or read: a warp each at the least, in whole blocks of warps, by a 31-bit index.
+constexpr int kMaxTokens = 0x7fffff00;
+
 // Present (or, with heads 0, absent) and aligned to one element.
 int check_heads(const kint_heads* h, int dtype) {
   if (!h || h->heads < 0 || (h->heads > 0 && !h->ptr)) return KINT_ERR_ARG;
+  if (h->heads > kMaxHeads) return KINT_ERR_UNSUPPORTED;
   return reinterpret_cast<uintptr_t>(h->ptr) % elem_size(dtype) ? KINT_ERR_ALIGN : KINT_OK;
 }
 Heads heads_of(const kint_heads* h) {
@@ -203,7 +208,8 @@ int kint_rope(const kint_heads* q, const kint_heads* q_out, const kint_heads* k,
   if (q->heads != q_out->heads || k->heads != k_out->heads || q->heads + k->heads < 1) return KINT_ERR_ARG;
   if ((rc = check_rotation(pos, table, max_pos, rot, d))) return rc;
   // (one work item a chunk of 1 to 16 channels of a token at the least: a 31-bit index)
-  if ((long long)B * T * ((d + 1) / 2 + 1) * ((q->heads + k->heads + 7) / 8) > 0x7fff0000ll) return KINT_ERR_UNSUPPORTED;
+  const long long most = 0x7fff0000ll / (((d + 1) / 2 + 1) * (long long)((q->heads + k->heads + 7) / 8));
+  if ((long long)B * T > most) return KINT_ERR_UNSUPPORTED;
   RopeP p;
   if ((rc = serve_device(&p.status))) return rc;
   if (B == 0 || T == 0) return KINT_OK;
@@ -229,6 +235,7 @@ int kint_cache_append(const kint_cache* cache, const kint_heads* k, const kint_h
   }
   if (table && (rc = check_rotation(pos, table, max_pos, rot, cache->d))) return rc;
   if (reinterpret_cast<uintptr_t>(slots) % 8) return KINT_ERR_ALIGN;
+  if (tokens > kMaxTokens) return KINT_ERR_UNSUPPORTED;
   CacheIoP p;
   if ((rc = serve_device(&p.status))) return rc;
   if (tokens == 0) return KINT_OK;
@@ -248,6 +255,7 @@ int kint_cache_read(const kint_cache* cache, const int64_t* slots, int tokens, c
   for (const kint_heads* h : {k, v})
     if (h && ((rc = check_heads(h, dtype)) || (rc = h->heads == cache->kv_heads ? KINT_OK : KINT_ERR_ARG))) return rc;
   if (reinterpret_cast<uintptr_t>(slots) % 8) return KINT_ERR_ALIGN;
+  if (tokens > kMaxTokens) return KINT_ERR_UNSUPPORTED;
   CacheIoP p;
   if ((rc = serve_device(&p.status))) return rc;
   if (tokens == 0) return KINT_OK;

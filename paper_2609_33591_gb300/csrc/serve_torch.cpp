@@ -67,6 +67,11 @@ int whole(PyObject* o) {
   need(v >= INT32_MIN && v <= INT32_MAX, "a whole number is out of range");
   return (int)v;
 }
+// A size as the C calls take it.
+int size(int64_t n) {
+  need(n <= INT32_MAX, "a size is past 2^31 - 1");
+  return (int)n;
+}
 // The call's stream: the current one, or the given handle, which is then the current one while the call allocates, so that
 // its memory belongs to it.
 struct CallStream {
@@ -100,7 +105,7 @@ kint_heads heads(const at::Tensor& t, const char* what, int dims) {
     throw Refused();
   }
   type_of(t, what);
-  return kint_heads{t.data_ptr(), dims == 4 ? t.stride(0) : 0, t.stride(-3), t.stride(-2), (int)t.size(-2)};
+  return kint_heads{t.data_ptr(), dims == 4 ? t.stride(0) : 0, t.stride(-3), t.stride(-2), size(t.size(-2))};
 }
 // Whole numbers on the GPU, contiguous in the last dimension.
 template <class I>
@@ -115,11 +120,11 @@ I* ints(const at::Tensor& t, const char* what) {
 // pages [num_blocks, kv_heads, block_size / 16, 18 d], uint8; blocks may be strided.
 kint_cache pool(const at::Tensor& t) {
   need(t.is_cuda() && t.scalar_type() == at::kByte && t.dim() == 4, "pages: expected a 4-D uint8 CUDA tensor");
-  const int64_t slabs = t.size(2), size = t.size(3);
-  need(size % 18 == 0 && t.stride(3) == 1 && t.stride(2) == size && t.stride(1) == slabs * size,
+  const int64_t slabs = t.size(2), bytes = t.size(3);
+  need(bytes % 18 == 0 && t.stride(3) == 1 && t.stride(2) == bytes && t.stride(1) == slabs * bytes,
        "pages: expected [num_blocks, kv_heads, block_size / 16, 18 d], contiguous within a block");
   need(t.size(0) <= INT32_MAX && slabs <= 4096, "pages: too many blocks or slabs");
-  return kint_cache{t.data_ptr(), t.stride(0), (int)t.size(0), 16 * (int)slabs, (int)t.size(1), (int)(size / 18)};
+  return kint_cache{t.data_ptr(), t.stride(0), (int)t.size(0), 16 * (int)slabs, size(t.size(1)), size(bytes / 18)};
 }
 struct Table {
   const float* ptr = nullptr;
@@ -128,7 +133,7 @@ struct Table {
 Table rotations(const at::Tensor& t) {
   need(t.is_cuda() && t.scalar_type() == at::kFloat && t.dim() == 3 && t.size(2) == 2 && t.is_contiguous(),
        "table: expected a contiguous fp32 CUDA tensor [max_pos, rot / 2, 2]");
-  return Table{static_cast<const float*>(t.data_ptr()), (int)t.size(0), 2 * (int)t.size(1)};
+  return Table{static_cast<const float*>(t.data_ptr()), size(t.size(0)), size(2 * t.size(1))};
 }
 
 // A tensor over part of `base`'s memory, `at` elements of its own type in, without a dispatched view: results that come
@@ -221,7 +226,7 @@ PyObject* extend_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
                   at_cu = at_lens + B, at_free = at_cu + B + 1, at_ref = at_free + 1;
     const at::Tensor out = at::empty({at_ref + 1}, lens.options());
     int32_t* o = static_cast<int32_t*>(out.data_ptr());
-    run(api.blocks_extend(pl, pa, pt, (int)table.stride(0), (int)table.size(1), pf, (int)list.numel(), pn, (int)B, block, tokens,
+    run(api.blocks_extend(pl, pa, pt, size(table.stride(0)), size(table.size(1)), pf, size(list.numel()), pn, size(B), block, tokens,
                           o + at_lens, o + at_free, o + at_cu, reinterpret_cast<int64_t*>(o), o + at_pos, o + at_req, o + at_ref,
                           stream.handle),
         "kint_blocks_extend");
@@ -265,7 +270,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
          "out disagrees with q and k");
     if (q.numel() || (k && k->numel())) {
       const kint_heads ho = heads(qo, "out", 4), hko = k ? heads(ko, "out", 4) : kint_heads{};
-      run(api.rope(&hq, &ho, &hk, &hko, pp, pos.dim() == 2 ? pos.stride(0) : 0, tab.ptr, tab.max_pos, (int)B, (int)T, (int)q.size(3),
+      run(api.rope(&hq, &ho, &hk, &hko, pp, pos.dim() == 2 ? pos.stride(0) : 0, tab.ptr, tab.max_pos, size(B), size(T), size(q.size(3)),
                    tab.rot, PyObject_IsTrue(a[4]), PyObject_IsTrue(a[5]), type_of(q, "q"), stream.handle),
           "kint_rope");
       if (!none(a[6])) {
@@ -319,7 +324,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       }
     }
     if (tokens) {
-      run(api.append(&c, &hk, &hv, ints<int64_t>(slots, "slots"), (int)tokens, turn ? &hq : nullptr, turn ? &hqo : nullptr, pos, tab.ptr,
+      run(api.append(&c, &hk, &hv, ints<int64_t>(slots, "slots"), size(tokens), turn ? &hq : nullptr, turn ? &hqo : nullptr, pos, tab.ptr,
                      tab.max_pos, tab.rot, PyObject_IsTrue(a[7]), type_of(k, "k"), stream.handle),
           "kint_cache_append");
       wrote(pages);
@@ -351,7 +356,7 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
                      v = part(both, both.scalar_type(), each, {slots.size(0), c.kv_heads, c.d}, {});
     if (slots.size(0)) {
       const kint_heads hk = heads(k, "k", 3), hv = heads(v, "v", 3);
-      run(api.read(&c, ps, (int)slots.size(0), &hk, &hv, (kint_dtype)type, stream.handle), "kint_cache_read");
+      run(api.read(&c, ps, size(slots.size(0)), &hk, &hv, (kint_dtype)type, stream.handle), "kint_cache_read");
     }
     return Py_BuildValue("(NN)", wrap(k), wrap(v));
   });
@@ -368,9 +373,9 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
              cu.size(0) == lens.size(0) + 1,
          "q, pages, table, lens and cu disagree");
     const int32_t *pt = ints<int32_t>(table, "table"), *pl = ints<int32_t>(lens, "lens"), *pc = ints<int32_t>(cu, "cu");
-    const int window = whole(a[9]), sinks = whole(a[10]), B = (int)lens.size(0), width = (int)table.size(1);
+    const int window = whole(a[9]), sinks = whole(a[10]), B = size(lens.size(0)), width = size(table.size(1));
     const int64_t hold = (int64_t)width * c.block_size;
-    const int max_new = none(a[11]) ? (int)q.size(0) : whole(a[11]);
+    const int max_new = none(a[11]) ? size(q.size(0)) : whole(a[11]);
     const int max_len = none(a[12]) ? (int)(hold < INT32_MAX ? hold : INT32_MAX) : whole(a[12]);
     const double tau = PyFloat_AsDouble(a[7]);
     if (tau == -1.0 && PyErr_Occurred()) throw Refused();
@@ -398,7 +403,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         ws = tensor(a[14], "ws");
         need(ws.is_cuda() && ws.is_contiguous(), "ws: expected a contiguous CUDA tensor");
       }
-      run(api.attn(&hq, &ho, &c, pt, (int)table.stride(0), width, pl, pc, (int)q.size(0), B, window, sinks, whole(a[5]), (kint_calib)whole(a[6]),
+      run(api.attn(&hq, &ho, &c, pt, size(table.stride(0)), width, pl, pc, size(q.size(0)), B, window, sinks, whole(a[5]), (kint_calib)whole(a[6]),
                    (float)tau, (kint_recon)whole(a[8]), max_new, max_len, type_of(q, "q"), slots, none(a[13]), ws.data_ptr(), ws.is_same(pages) ? kUnusedWorkspace : ws.nbytes(),
                    stream.handle),
           "kint_cache_attn");

@@ -230,3 +230,12 @@ def test_a_free_list_of_rows_is_refused():
         with pytest.raises(ValueError, match="free"):
             serve.extend_blocks(lens, new, table, free, n_free, 16, 3)
     assert table.tolist() == [[-1]]
+
+
+def test_sizes_past_31_bits_are_refused():
+    """Not taken modulo 2^32 (here 2^32 + 2 heads on top of each other as 2)."""
+    x = torch.ones(1, 1, 1, 64, device="cuda")
+    many = x.expand(1, 1, (1 << 32) + 2, 64)
+    with pytest.raises(ValueError, match="past 2"):
+        serve.rope(many, None, ints([1]), serve.rope_table(4, 64), out=(many, None))
+    assert (x == 1).all()

@@ -24,3 +24,26 @@ def test_more_rows_or_units_than_an_index_holds(sizes):
 def test_the_most_rows_that_an_index_holds():
     f = serve.load().kint_cache_attn_workspace_bytes
     assert f(1, 64, 1, 64, 0, 0, 1 << 24, 256) > 0
+
+
+ROPE = dict(q=heads(), qo=heads(), k=heads(0), ko=heads(0), pos=P, sb=0, table=P, max_pos=8, B=1, T=8, d=64, rot=64, il=0, inv=0, dtype=1,
+            stream=None)
+MOST = (1 << 31) - 1
+
+
+@pytest.mark.parametrize("kw", [
+    dict(q=heads(MOST - 2), qo=heads(MOST - 2)),                                          # groups of 8 heads past 2^31
+    dict(q=heads(1 << 30), qo=heads(1 << 30), k=heads(1 << 30), ko=heads(1 << 30)),       # heads of both past 2^31
+    dict(B=MOST, T=MOST, q=heads(1 << 24), qo=heads(1 << 24)),                            # work items past 2^63
+    dict(B=1 << 16, T=1 << 15),
+])
+def test_rotations_of_more_items_than_an_index_holds(kw):
+    assert serve.load().kint_rope(*{**ROPE, **kw}.values()) == -2
+
+
+@pytest.mark.parametrize("tokens", [MOST, MOST - 6])
+def test_more_cached_tokens_than_an_index_holds(tokens):
+    """A warp a token: the last block's warps are numbered past the last token."""
+    lib = serve.load()
+    assert lib.kint_cache_append(cache(), heads(), heads(), P, tokens, None, None, None, None, 0, 0, 0, 0, None) == -2
+    assert lib.kint_cache_read(cache(), P, tokens, heads(), None, 0, None) == -2
