@@ -1028,10 +1028,10 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   pdl_wait();
   bool bad = false;
   const int C = p.nsplit, id = blockIdx.x / C, rank = blockIdx.x - id * C;
-  const int2 ends = row_ends(p);
   const Unit u = unit_of(p, id, R, bad, reinterpret_cast<uint32_t*>(big));
-  fill_rows<D>(p, u, ends, bad, rank == 0);
+  const int2 ends = row_ends(p);
   if (u.n == 0) {  // nothing to see, for every block of the cluster
+    fill_rows<D>(p, u, ends, bad, rank == 0);
     if (rank == 0) store_zeros(p, u, D);
     if (bad) dev_flag(p.status, DEV_ERR_BOUNDS);
     return;
@@ -1043,6 +1043,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 2 && D == 128) ? 12 / kWarps 
   const Ring<D> ring(sm4);
   {
     ring.template prime<true>(sh);
+    fill_rows<D>(p, u, ends, bad, rank == 0);
     if (MODE == M_GRID && threadIdx.x <= p.Kint && p.calib != CAL_MINMAX) grid[threadIdx.x] = p.e[threadIdx.x];
     q.store(p, qt, reinterpret_cast<__half (*)[R][D + 8]>(big));
     __syncthreads();
