@@ -23,7 +23,10 @@
  *   - Tensors of queries, keys, values and outputs are fp32, bfloat16 or fp16 (one type
  *     a call) with any strides over batch, time and head and contiguous channels
  *     (kint_heads); they need the alignment of one element only.
- *   - Sums, row statistics and weights are fp32.
+ *   - Sums, row statistics and weights are fp32.  Scores are taken to be finite and below 0.9e38 in magnitude, and bfloat16 queries
+ *     below 2^120.
+ *   - Sizes have to fit their kernels' 32-bit indices: KINT_ERR_UNSUPPORTED past 2^30 rows (new tokens times query heads) a kv head, 2^30
+ *     units (request, kv head, row tile), 2^24 heads, 2^31 - 256 tokens an append or read.
  *
  * The cache.  A pool of num_blocks blocks of block_size tokens (a power of two, 16 to
  * 4096); block n of the pool starts at pages + n * block_stride bytes and holds, for
@@ -136,7 +139,7 @@ int kint_cache_read(const kint_cache* cache, const int64_t* slots, int tokens, c
  *   Kint, calib, tau, recon: the weights, as for kint_attn_fwd (the hard forward under Nearest); the grid is
  *   anchored at the row's extrema over the keys it sees.
  *   max_new  bound on cu[b + 1] - cu[b]; max_len bound on lens[b] (<= width * block_size): they size the launch and
- *            the workspace; rows or keys past them are left out and flagged, and so are requests whose rows do not lie
+ *            the workspace (with loose bounds both grow: every row that could be there has its place); rows or keys past them are left out and flagged, and so are requests whose rows do not lie
  *            within 0 .. rows.
  *   workspace: kint_cache_attn_workspace_bytes bytes (16-byte aligned).  256 bytes are asked for, and not touched, where the
  *            scores fit the shared memory of one launch.

@@ -76,7 +76,9 @@ struct AttnPlan {
 };
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 constexpr int kSms = 152;
-constexpr int kBlocksPerSm = 16 / kAttnWarps;          // of at most 128 registers a thread
+// Of at most 128 registers a thread.  (By registers: with 32 KB of scores, heads of 128 and four rows, MinMax's tables at K >= 11
+// leave room for three.  Clusters planned as one wave then take two, and a cooperative launch that does not fit two launches.)
+constexpr int kBlocksPerSm = 16 / kAttnWarps;
 constexpr int kBlockSlabs = 32 * kAttnWarps;           // a warp keeps the addresses of 32
 constexpr int kMinSlabs = 2 * kAttnWarps;              // fewest slabs a block that splitting a unit over a cluster leaves
 constexpr int kMinCoop = 8 * kAttnWarps;               // and over a cooperative launch

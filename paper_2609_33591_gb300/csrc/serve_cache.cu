@@ -1,7 +1,8 @@
 // Writing tokens into the 4-bit cache and reading them back (format: kint_serve.h).
 //
-// A group of 64 channels keeps lo and hi as s = fp16((hi - lo) / 15), c = fp16(lo + 8 s)
-// and each channel as clamp(rint((x - c) / s), -8, 7): 0.5625 bytes a channel.  Both
+// A group of 64 channels keeps lo and hi as s = fp16((hi - lo) * fp32(1 / 15)), c = fp16(lo + 8 s)
+// and each channel as clamp(rint((x - c) * (1 / s)), -8, 7), products and not quotients, so that every writer rounds alike:
+// 0.5625 bytes a channel.  Both
 // kernels move each byte once and are bound by HBM on prompts, by latency on one step's
 // tokens.  A lane holds eight channels (one K word, two halves of V words; 16 bytes of a
 // 16-bit input), so a group is eight lanes and its extrema three butterfly steps, and a

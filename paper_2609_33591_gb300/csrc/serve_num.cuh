@@ -27,18 +27,7 @@ struct alignas((sizeof(E) * N) < 16 ? (sizeof(E) * N) : 16) Vec {
   E v[N];
 };
 
-// N consecutive channels from x: one vector access when `vec` (the address is a multiple of the vector), else one by one.
-template <class E, int N>
-__device__ __forceinline__ void load_ch(const E* x, bool vec, float (&f)[N]) {
-  if (vec) {
-    const Vec<E, N> a = *reinterpret_cast<const Vec<E, N>*>(x);
-#pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = to_f32(a.v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = to_f32(x[i]);
-  }
-}
+// N consecutive channels to x: one vector access when `vec` (the address is a multiple of the vector), else one by one.
 template <class E, int N>
 __device__ __forceinline__ void store_ch(E* x, bool vec, const float (&f)[N]) {
   if (vec) {

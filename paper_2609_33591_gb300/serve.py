@@ -127,9 +127,10 @@ def rope_frequencies(rot: int, base: float = 10000.0, *, scaling: str | None = N
 
     scaling, for contexts longer than those trained on (original_len tokens, longer by ``factor``):
       None      the plain angles;
-      "linear"  every angle / factor (positions interpolated);
-      "base"    base * factor^(rot / (rot - 2)): the slowest pair turns 1 / factor as far, the fastest as before;
-      "bands"   pairs that turn less than ``slow`` times over original_len are divided by factor, those that turn more
+      "linear"  every angle / factor (position interpolation, Chen et al. 2023);
+      "base"    base * factor^(rot / (rot - 2)): the slowest pair turns 1 / factor as far, the fastest as before (known as
+                NTK-aware scaling);
+      "bands"   (YaRN, Peng et al. 2023) pairs that turn less than ``slow`` times over original_len are divided by factor, those that turn more
                 than ``fast`` times are kept, a linear blend between; magnitude 0.1 ln(factor) + 1.
     """
     _need(rot >= 2 and rot % 2 == 0, "rot must be even and at least 2")
@@ -217,7 +218,8 @@ def attention(q, pages, table, lens, cu, cfg: kint.Config, *, window: int = 0, s
     """K-interval attention of new tokens over the cache: q [rows, heads, d], request b's rows cu[b] .. cu[b + 1] - 1 at
     the last positions of its lens[b] cached tokens, whose blocks are table[b].  window > 0: a row sees its last
     ``window`` keys and the first ``sinks``.  max_new and max_len bound the rows a request has and lens (host numbers
-    that size the launch; by default rows and what the table can hold).  ``slots``: the plan's, so that requests it refused
+    that size the launch and its scratch; by default rows and what the table can hold, so give max_new = 1 when every request has one
+    token: for 64 of them, 32 heads over 8 and a table of 32768 tokens, 0.3 GB of scratch and not 18.3).  ``slots``: the plan's, so that requests it refused
     get zeros (without them their rows are taken for the last positions of what is cached).  Rows that are no request's, or left out for
     their bounds, are zero in a new output and left as they are in ``out``."""
     return (_mod or _ext()).attention(q, pages, table, lens, cu, cfg.Kint, cfg.calib, cfg.tau, cfg.recon, window, sinks, max_new,
@@ -265,7 +267,7 @@ class PagedCache:
 class KIntServingAttention(KIntSelfAttention):
     """The GPT-2 K-interval attention block with rotary positions: ``forward`` as in training (whole sequences, rotation
     and attention differentiable), ``step`` for new tokens over a 4-bit paged cache.  The cache has as many kv heads as
-    the block has heads; weights are KIntSelfAttention's."""
+    the block has heads; weights are KIntSelfAttention's.  Sequences and the bound on a step's lengths have to lie within max_pos."""
 
     def __init__(self, n_embd: int = 768, n_head: int = 12, cfg: kint.Config | None = None, *, max_pos: int = 4096,
                  rot: int | None = None, base: float = 10000.0, interleaved: bool = False, window: int = 0, sinks: int = 0,
@@ -301,7 +303,8 @@ class KIntServingAttention(KIntSelfAttention):
     def step(self, x, cache: PagedCache, plan: BlockPlan, layer: int = 0, *, max_new: int | None = None,
              max_len: int | None = None):
         """x [rows, C]: the new tokens of every request in the plan's order (cache.extend).  Places left over and requests that
-        the plan refused get the projection of zeros."""
+        the plan refused get the projection of zeros.  max_new and max_len as in ``attention``: by default all rows, and the
+        cache's max_len."""
         rows, C = x.shape
         D = C // self.n_head
         max_len = max_len or cache.max_len
