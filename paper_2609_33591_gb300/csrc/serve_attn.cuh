@@ -341,15 +341,20 @@ __device__ __forceinline__ void zero_row(const AttnP& p, int row, int head, int 
     store_o(p, row * p.o.st + (head + x / (D / 4)) * p.o.sh + 4 * (x % (D / 4)), z);
 }
 template <int D>
-__device__ __forceinline__ void fill_rows(const AttnP& p, const Unit& u, int2 ends, bool bad, bool lead) {
-  const int from = min(max(ends.x, 0), p.rows), to = min(max(ends.y, 0), p.rows);
+__device__ __noinline__ void zero_rest(const AttnP& p, int from, int to, int b, int h, bool lost) {  // (out of the kernels' way)
   const long long rest = (long long)from + (p.rows - to);
   for (long long r = blockIdx.x; r < rest; r += gridDim.x) zero_row<D>(p, (int)(r < from ? r : to + (r - from)), 0, p.o.n);
-  if (p.fill && bad && lead && u.row0 == 0) {
-    const int next = __ldg(p.cu + u.b + 1), add = next - u.first;
-    const bool there = u.first >= 0 && add >= 0 && u.first <= p.rows - add;
-    for (int r = there ? u.first + min(add, p.max_new) : max(u.first, 0); r < min(next, p.rows); ++r) zero_row<D>(p, r, u.h * p.G, p.G);
+  if (lost) {
+    const int first = __ldg(p.cu + b), next = __ldg(p.cu + b + 1), add = next - first;
+    const bool there = first >= 0 && add >= 0 && first <= p.rows - add;
+    for (int r = there ? first + min(add, p.max_new) : max(first, 0); r < min(next, p.rows); ++r) zero_row<D>(p, r, h * p.G, p.G);
   }
+}
+template <int D>
+__device__ __forceinline__ void fill_rows(const AttnP& p, const Unit& u, int2 ends, bool bad, bool lead) {
+  const int from = min(max(ends.x, 0), p.rows), to = min(max(ends.y, 0), p.rows);
+  const bool lost = p.fill && bad && lead && u.row0 == 0;
+  if (from > 0 || to < p.rows || lost) zero_rest<D>(p, from, to, u.b, u.h, lost);
 }
 
 // Where a row of the tile lives.
