@@ -45,7 +45,7 @@
 // of eight (2048 units of 256 keys: 50 -> 35 us).  Measured on a GB300: 64 requests of 1021 to 8192 keys, 8 kv heads of 128,
 // bf16, FWM Nearest (347 MB) 93 us = 3.7 TB/s, 55% of the measured copy rate (a read of such slabs without arithmetic: 67 us
 // for 302 MB); one request of 131071 keys, MinMax (151 MB), cooperative, 41 us; four new tokens a request in windows of 1024
-// keys (19 MB) 18 us; 8 requests of up to 1024 keys, 12 heads of 64, fp32 (4.3 MB) 9 us; one of 333 keys, 24 heads 5.8 us.
+// keys (19 MB) 18 us; 8 requests of up to 1024 keys, 12 heads of 64, fp32 (4.3 MB) 9 us; one of 333 keys, 24 heads 6.1 us.
 // Writing zeros where no request answers, and a NaN value that is seen counting whatever its weight, cost 1% of the first.
 #pragma once
 #include <atomic>

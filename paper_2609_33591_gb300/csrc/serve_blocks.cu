@@ -8,7 +8,7 @@
 // Traffic is 16 bytes a token written and little else, so small steps are bound by
 // latency: one launch, in which every CTA forms both prefix sums over all requests by
 // itself (8 bytes a request from L2) instead of a scan launch followed by an expansion, and expands 4096 tokens or more.
-// Measured on a GB300: 1024 requests with 1.03 million new tokens (16.9 MB) 9.5 us, bound by instruction issue (56% of the slots, a
+// Measured on a GB300: 1024 requests with 1.03 million new tokens (16.9 MB) 9.5 us, bound by instruction issue (57% of the slots, a
 // bisection for every four tokens) behind the scans; 256 requests with one token each 5.5 us, of which about 2 are any launch's; several waves of blocks were slower (11.3 us), since each block sums all requests again.
 #include "serve_params.h"
 #include "tc.cuh"
