@@ -303,12 +303,14 @@ class KIntServingAttention(KIntSelfAttention):
     def step(self, x, cache: PagedCache, plan: BlockPlan, layer: int = 0, *, max_new: int | None = None,
              max_len: int | None = None):
         """x [rows, C]: the new tokens of every request in the plan's order (cache.extend).  Places left over and requests that
-        the plan refused get the projection of zeros.  max_new and max_len as in ``attention``: by default all rows, and the
-        cache's max_len."""
+        the plan refused get the projection of zeros.  max_new and max_len as in ``attention``: by default all rows, and
+        what the cache's table holds."""
         rows, C = x.shape
         D = C // self.n_head
-        max_len = max_len or cache.max_len
-        _need(max_len <= self.rope.size(0), f"requests of up to {max_len} tokens are past the layer's max_pos, {self.rope.size(0)}")
+        most = self.rope.size(0)
+        _need((max_len or cache.max_len) <= most, f"requests of up to {max_len or cache.max_len} tokens are past the layer's max_pos, {most}")
+        # (by default what the table's blocks hold: the cache lets a request fill its last one)
+        max_len = max_len or min(cache.table.size(1) * cache.block_size, most)
         q, k, v = (t.view(rows, self.n_head, D) for t in self.c_attn(x).split(C, dim=1))
         pages = cache.pages[layer]
         q = append(k, v, plan.slots, pages, q=q, pos=plan.pos, table=self.rope, interleaved=self.interleaved)

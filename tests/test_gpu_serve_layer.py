@@ -103,3 +103,14 @@ def test_a_cache_takes_its_own_size_of_memory():
             serve.PagedCache(1, 1, 64, 4, 4, 64, **bad)
     with pytest.raises(kint.KintError):
         serve.PagedCache(1, 1, 64, 4, 4, 96)
+
+
+def test_a_request_may_fill_its_last_block():
+    """A table of blocks holds more than a max_len that is no multiple of them, and extend hands the rest out: every key is seen."""
+    torch.manual_seed(4)
+    layer = serve.KIntServingAttention(256, 4, kint.Config(Kint=8, calib=FWM, recon=kint.RECON_LERP), max_pos=128)
+    x = torch.randn(120, 256, device="cuda")
+    short, long = (serve.PagedCache(1, 1, n, 2, 4, 64, block_size=64) for n in (100, 128))
+    got, want = (torch.cat([layer.step(x[a:b], c, c.extend(ints([b - a]), b - a), max_new=b - a) for a, b in ((0, 90), (90, 119), (119, 120))])
+                 for c in (short, long))
+    assert short.lens.tolist() == [120] and torch.equal(got, want)
