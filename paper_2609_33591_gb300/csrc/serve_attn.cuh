@@ -27,10 +27,10 @@
 //   q . k = sum_groups s (q . n) + (c - 8 s) (sum of q),  P . v = (P s) . n + P (c - 8 s).
 // (The nibbles become fp16 numbers by or-ing them under the exponent of 1024 and subtracting, the published way to unpack 4-bit
 // weights: Kim et al. 2022, "Who Says Elephants Can't Run".)
-// For fp32 outputs the codes are centred first, n - 8 in fp16: sums of unsigned n cancel against 8 s
-// when many keys average out.  16-bit outputs take that in their fp32 sums, for the instructions it saves: over 131071 keys (bf16,
-// MinMax) the error against 64 bits is 1.69e-3 of the output's size, 1.67e-3 with fp32 sums rounded once, nearly all of
-// either the output's own rounding; in windows of 1024 keys (fp16) 2.11e-4 against 2.07e-4.
+// Sums of unsigned n cancel against 8 s when many keys average out.  For fp32 outputs the codes are centred first, n - 8 in fp16; for
+// 16-bit outputs, where that would cost instructions, every other slab of values enters as its codes' complement (value_pass):
+// over 131071 keys the error against 64 bits is then 2.12e-4 of the output's size in fp16 (softmax), 2.11e-4 with fp32 sums rounded
+// once, and 3.1e-4 with all slabs alike.
 // q is scaled by a power of two per row, to fp16 (one part for bfloat16 and fp16 queries: exact; two
 // for fp32: 22 bits).  P s is scaled by a power of two per unit, from the largest V scale (read in the
 // first pass), so that two fp16 parts keep it to 2^-23 of itself down to 2^-14 of its maximum, and to 2^-37 of that
@@ -73,18 +73,19 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The nibbles at bits 0 and 16, or at bits 4 and 20, as fp16 operands: n - 8 (CENTRED), else n 2^-24 and 16 n 2^-24.
+// The nibbles at bits 0 and 16, or at bits 4 and 20, as fp16 operands: n - 8 (CENTRED), else n 2^-24 and 16 n 2^-24; `flip`: of
+// 15 - n.
 template <bool CENTRED>
-__device__ __forceinline__ uint32_t code_low(uint32_t w) {
-  const uint32_t m = w & 0x000f000fu;
+__device__ __forceinline__ uint32_t code_low(uint32_t w, bool flip = false) {
+  const uint32_t m = (flip ? ~w : w) & 0x000f000fu;
   if constexpr (!CENTRED) return m;
   const uint32_t x = m | 0x64006400u;  // 1024 + n
   const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), __floats2half2_rn(1032.0f, 1032.0f));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 template <bool CENTRED>
-__device__ __forceinline__ uint32_t code_high(uint32_t w) {
-  const uint32_t m = w & 0x00f000f0u;
+__device__ __forceinline__ uint32_t code_high(uint32_t w, bool flip = false) {
+  const uint32_t m = (flip ? ~w : w) & 0x00f000f0u;
   if constexpr (!CENTRED) return m;
   const uint32_t x = m | 0x64006400u;  // 1024 + 16 n
   const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&x), __floats2half2_rn(0.0625f, 0.0625f),
@@ -216,6 +217,7 @@ __device__ __forceinline__ Share share_of(const AttnP& p, const Unit& u, int i0,
 template <int D>
 struct Ring {
   static constexpr int kStages = D == 128 ? 4 : 6, kPlace = 10 * D, kBytes = kWarps * kStages * kPlace;
+  static_assert(kStages % 2 == 0, "an item's place tells whether it is odd");
   uint32_t at;  // shared address of the warp's first place
 
   __device__ __forceinline__ explicit Ring(void* smem) : at(smem_u32(smem) + warp_id_uniform() * kStages * kPlace) {}
@@ -251,7 +253,7 @@ struct Ring {
       commit();
     }
   }
-  // work(l, shared address) for items 0 .. n - 1 in order.
+  // work(l, shared address, whether l is odd) for items 0 .. n - 1 in order.
   template <bool KEYS, class Work>
   __device__ __forceinline__ void stream(const Share& sh, Work work) const {
     for (int l = 0; l < sh.n; l += kStages) {
@@ -262,7 +264,7 @@ struct Ring {
           __syncwarp();  // item l + s is here for every lane, and the place of the one before it has been read
           if (l + s + kStages - 1 < sh.n) copy<KEYS>(sh, l + s + kStages - 1, (s + kStages - 1) % kStages);
           commit();
-          work(l + s, at + s * kPlace);
+          work(l + s, at + s * kPlace, (s & 1) != 0);
         }
     }
   }
@@ -506,7 +508,7 @@ __device__ __forceinline__ void key_pass(const AttnP& p, const Unit& u, const QT
   const int out0 = score_row(2 * t, four), out1 = score_row(2 * t + 1, four);
   float* out = scores + (size_t)warp_id_uniform() * p.slab_words;
   __half2 vs = __floats2half2_rn(0.0f, 0.0f);  // (s, c); only s counts
-  ring.template stream<true>(sh, [&](int l, uint32_t at) {
+  ring.template stream<true>(sh, [&](int l, uint32_t at, bool) {
     KeyRegs<D> r;
     load_keys<D>(at, r);
     float s[NT][4];
@@ -783,7 +785,10 @@ __device__ __forceinline__ void value_pass(const AttnP& p, const Share& sh, cons
   }
   const float* in0 = scores + (size_t)warp_id_uniform() * p.slab_words;
   const int k0 = score_at(in, 2 * t), k1 = score_at(in, 2 * t + 8);
-  ring.template stream<false>(sh, [&](int l, uint32_t at) {
+  ring.template stream<false>(sh, [&](int l, uint32_t at, bool odd) {
+    // Uncentred codes sum up to some 8 s times the weights, which the centres take off again; the products' fp32 sums round towards
+    // zero, by that large sum's units.  So every other slab enters as -P s times 15 - n: the sums then stay near zero.
+    const bool flip = !F32 && odd;
     ValueRegs<D> r;
     load_values<D>(at, r);
     const bool all = (sh.full >> l) & 1u;
@@ -799,11 +804,16 @@ __device__ __forceinline__ void value_pass(const AttnP& p, const Share& sh, cons
     for (int k = 0; k < NG; ++k) {
       // (s, c) of the four keys, as pairs of keys
       const float2 f0 = scale_of(r.sa[k]), f1 = scale_of(r.sa[NG + k]), f2 = scale_of(r.sb[k]), f3 = scale_of(r.sb[NG + k]);
-      const float2 s0 = make_float2(f0.x, f1.x), s1 = make_float2(f2.x, f3.x);
+      float2 s0 = make_float2(f0.x, f1.x), s1 = make_float2(f2.x, f3.x);
       float2 c0 = make_float2(f0.y, f1.y), c1 = make_float2(f2.y, f3.y);
-      if constexpr (!F32) {
-        c0 = fma2(make_float2(-8.0f, -8.0f), s0, c0);
-        c1 = fma2(make_float2(-8.0f, -8.0f), s1, c1);
+      if constexpr (!F32) {  // P v = P s n + P (c - 8 s) = -P s (15 - n) + P (c + 7 s)
+        const float mid = flip ? 7.0f : -8.0f;
+        c0 = fma2(make_float2(mid, mid), s0, c0);
+        c1 = fma2(make_float2(mid, mid), s1, c1);
+        if (flip) {
+          s0 = make_float2(-s0.x, -s0.y);
+          s1 = make_float2(-s1.x, -s1.y);
+        }
       }
       uint32_t b0[NT][2], b1[NT][2];
 #pragma unroll
@@ -830,7 +840,7 @@ __device__ __forceinline__ void value_pass(const AttnP& p, const Share& sh, cons
       for (int jj = 0; jj < 4; ++jj) {
         const int wi = 2 * k + (jj >> 1);
         const uint32_t xa = jj & 1 ? r.va[wi] >> 8 : r.va[wi], xb = jj & 1 ? r.vb[wi] >> 8 : r.vb[wi];
-        const uint32_t a0 = code_low<F32>(xa), a1 = code_high<F32>(xa), a2 = code_low<F32>(xb), a3 = code_high<F32>(xb);
+        const uint32_t a0 = code_low<F32>(xa, flip), a1 = code_high<F32>(xa, flip), a2 = code_low<F32>(xb, flip), a3 = code_high<F32>(xb, flip);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll

@@ -97,3 +97,24 @@ def test_captured(way, requests, heads, calib, K, max_len):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(res, want)
+
+
+@pytest.mark.parametrize("heads", [4, 8, 16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("calib", [SOFT, MM])
+def test_rounding_of_long_sums(calib, d, heads):
+    """Over 131071 keys the values average out to a hundredth of themselves.  The result in fp16 is then off by its own rounding and
+    no more: within a tenth of the error of the 64-bit result rounded once (fp32 sums add some 2^-24 of the values, a hundredth of
+    an fp16 unit of such a result, to each)."""
+    n, g = 131071, torch.Generator(device="cuda").manual_seed(d + heads)
+    pages, slots = serve.cache_pages(128, 1024, 1, d), torch.arange(n, device="cuda")
+    k, v, q = (torch.randn(m, h, d, device="cuda", generator=g).half() for m, h in ((n, 1), (n, 1), (1, heads)))
+    serve.append(k, v, slots, pages)
+    cfg = kint.Config(Kint=8, calib=calib, recon=LERP)
+    table = torch.arange(128, dtype=torch.int32, device="cuda")[None]
+    o = serve.attention(q, pages, table, ints([n]), ints([0, 1]), cfg, max_new=1, max_len=n)[0].double()
+    k, v = (x[:, 0].double() for x in serve.read(pages, slots))
+    s = q[0].double() @ k.T / d ** 0.5
+    w = torch.stack([ref.weights((x - x.max()).cpu(), cfg) for x in s]).cuda()
+    want = w @ v / w.sum(-1, keepdim=True)
+    assert (o - want).norm() <= 1.1 * (want.half().double() - want).norm()
